@@ -1,0 +1,42 @@
+// Launchers of the operators of sp_ops.h, for their C entries and for the forward of students that use them.  They check nothing
+// that the entries check.
+#pragma once
+
+#include "sp_internal.h"
+#include "sp_ops.h"
+
+namespace sp {
+
+// Whether the n0 x n1 rows of `width` elements at strides s0 and s1 share no memory (the stride of a single row does not matter).
+inline bool rows_apart(int64_t n0, int64_t s0, int64_t n1, int64_t s1, int64_t width)
+{
+    if (n0 <= 1 || n1 <= 1) return (n0 <= 1 || s0 >= width) && (n1 <= 1 || s1 >= width);
+    return s0 < s1 ? s0 >= width && s1 >= (n0 - 1) * s0 + width : s1 >= width && s0 >= (n1 - 1) * s1 + width;
+}
+
+hipError_t launch_rotary(const void* x, int64_t xt, int64_t xh, void* out, int64_t ot, int64_t oh, int dtype, int tokens,
+                         int heads, int width, int dim, int layout, const double* freq, float factor, const int32_t* pos,
+                         const int32_t* cu, int batch, hipStream_t s);
+
+// codes [rows][c_row]: `width` of them, then zeros up to `padded`
+hipError_t launch_quantize_int8(const void* x, int64_t x_row, int dtype, int rows, int width, int8_t* codes, int64_t c_row, int padded,
+                                float* scales, hipStream_t s);
+
+// out[t][n] = epilogue(sum_k A[t][k] W[n][k] * a_scales[t] w_scales[n] + bias[n]) for k < groups students, each `_ss` behind the one before.
+struct Int8Args {
+    const int8_t* A;                    // [tokens][a_row], zero from Kd to a_row (a multiple of 128)
+    const float* a_scales;
+    const int8_t* W;                    // [N][w_row]
+    const float *w_scales, *bias;       // bias may be null
+    const void* res;                    // may be null
+    void* out;
+    int64_t a_row, w_row, res_row, out_row;
+    size_t a_ss, as_ss, w_ss, ws_ss, b_ss, res_ss, out_ss;      // bytes
+    int tokens, N, Kd, groups;
+};
+hipError_t launch_gemm_int8(const Int8Args& a, int dtype, int epilogue, hipStream_t s);
+
+size_t attend_workspace_bytes(const sp_attention_args& a);
+hipError_t launch_attend(const sp_attention_args& a, void* workspace, hipStream_t s);
+
+}  // namespace sp

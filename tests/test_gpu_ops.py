@@ -1,0 +1,560 @@
+"""The operators of include/sp_ops.h on the GPU against the 64-bit oracle (bounds are derived there, not fitted)."""
+import itertools
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import sp_ops_oracle as oracle
+from paper_2408_12526_amd import ops, sp
+
+pytestmark = pytest.mark.gpu
+TYPES = {"bf16": torch.bfloat16, "fp32": torch.float32}
+
+
+def dev(a, dtype=None):
+    t = torch.from_numpy(np.ascontiguousarray(a)).cuda()
+    return t if dtype is None else t.to(TYPES[dtype])
+
+
+def host(t):
+    return t.float().cpu().numpy()
+
+
+def near(got, want, bound, what=""):
+    got = got.double().cpu().numpy()
+    same = (np.isnan(want) & np.isnan(got)) | (got == want)
+    off = np.where(same, 0.0, np.abs(np.where(same, 0.0, got) - np.where(same, 0.0, want)))
+    bad = ~same & ~(off <= bound)
+    assert not bad.any(), f"{what}: {bad.sum()} of {bad.size}, worst {off[bad].max()} at {np.argwhere(bad)[0]}, bound {bound[tuple(np.argwhere(bad)[0])]}"
+
+
+# ---- 8-bit integers ---------------------------------------------------------------------------------------------
+
+def weights(rng, n, k):
+    w, s = ops.quantize_int8(dev(rng.standard_normal((n, k)).astype(np.float32) * 0.05))
+    return w, s
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("rows,width", [(1, 1), (3, 15), (5, 16), (7, 777), (130, 64), (2, 4096), (3, 5000), (4, 4113)])
+def test_quantize(dtype, rows, width):
+    rng = np.random.default_rng(rows * 7 + width)
+    x = dev(rng.standard_normal((rows, width)).astype(np.float32) * 10.0 ** rng.integers(-6, 6, (rows, 1)).astype(np.float32), dtype)
+    codes, scales = ops.quantize_int8(x)
+    c, s = oracle.quantize(host(x))
+    assert np.array_equal(codes.cpu().numpy(), c)
+    assert np.array_equal(scales.double().cpu().numpy(), s)
+
+
+def test_quantize_special_rows():
+    x = np.zeros((9, 40), np.float32)
+    x[1, 3], x[2, 39], x[3, 0] = np.inf, np.nan, -np.inf
+    x[4] = 2.0 ** -101
+    x[5, 7] = 2.0 ** -100
+    x[6, :4] = [127, 63.5, -62.5, 0.5]                      # halves go to the even code
+    x[7, 1] = 3.4e38
+    x[8, :2] = [1.0, 0.5]                                   # half of the largest: 63.5 before the roundings
+    codes, scales = ops.quantize_int8(dev(x))
+    c, s = oracle.quantize(x)
+    assert np.array_equal(codes.cpu().numpy(), c)
+    assert np.array_equal(scales.double().cpu().numpy(), s, equal_nan=True)
+    assert list(c[6, :4]) == [127, 64, -62, 0]
+
+
+def test_quantize_strided_and_in_place_width():
+    """Rows of a wider matrix, codes into a wider one: what stands behind the width stays."""
+    rng = np.random.default_rng(1)
+    wide = dev(rng.standard_normal((6, 100)).astype(np.float32))
+    codes, scales = torch.full((6, 64), 99, dtype=torch.int8, device="cuda"), torch.empty(6, device="cuda")
+    x = wide[:, 3:40]
+    rc = sp.raw_lib().sp_quantize_int8(x.data_ptr(), 100, sp.SP_DTYPE_FP32, 6, 37, codes.data_ptr(), 64, scales.data_ptr(),
+                                       torch.cuda.current_stream().cuda_stream)
+    assert rc == 0
+    c, s = oracle.quantize(host(x))
+    assert np.array_equal(codes[:, :37].cpu().numpy(), c) and bool((codes[:, 37:] == 99).all())
+    assert np.array_equal(scales.double().cpu().numpy(), s)
+
+
+LINEAR_SIZES = [(1, 1, 1), (1, 16, 3), (1, 768, 2304), (2, 100, 33), (5, 128, 64), (16, 1000, 129), (17, 257, 777), (31, 64, 1000), (33, 384, 256),
+                (63, 129, 65), (64, 1024, 512), (65, 127, 127), (128, 256, 128), (129, 640, 130), (200, 2048, 96), (257, 96, 300), (700, 130, 513), (1999, 72, 77)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("tokens,width_in,width_out", LINEAR_SIZES)
+def test_linear(dtype, tokens, width_in, width_out):
+    rng = np.random.default_rng(tokens + width_in * 3 + width_out)
+    w, ws = weights(rng, width_out, width_in)
+    x = dev(rng.standard_normal((tokens, width_in)).astype(np.float32), dtype)
+    bias = rng.standard_normal(width_out).astype(np.float32)
+    res = dev(rng.standard_normal((tokens, width_out)).astype(np.float32), dtype)
+    for how in ("plain", "bias", "gelu", "residual"):
+        b = None if how == "plain" else dev(bias)
+        r = res if how == "residual" else None
+        got = ops.linear_int8(x, w, ws, b, residual=r, gelu=how == "gelu")
+        want, bound = oracle.linear_int8(host(x), w.cpu().numpy(), ws.cpu().numpy(), None if b is None else bias,
+                                         None if r is None else host(r), how == "gelu", dtype)
+        near(got, want, bound, how)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("tokens", [1, 3, 70, 300])
+def test_linear_views(dtype, tokens):
+    """Rows of wider matrices on both sides; what stands beside the output stays; the output over the residual; padding of the weights'
+    rows holds anything."""
+    rng = np.random.default_rng(tokens)
+    K, N = 200, 150
+    xw = dev(rng.standard_normal((tokens, K + 33)).astype(np.float32), dtype)
+    x = xw[:, 5: 5 + K]
+    w, ws = weights(rng, N, K)
+    full = torch.full((N, 208 + 16), -77, dtype=torch.int8, device="cuda")
+    full[:, :K] = w
+    ow = torch.full((tokens, N + 9), 5.0, dtype=TYPES[dtype], device="cuda")
+    out = ow[:, 3: 3 + N]
+    out.copy_(dev(rng.standard_normal((tokens, N)).astype(np.float32)))
+    before = host(out)
+    ops.linear_int8(x, full[:, :K], ws, residual=out, out=out)
+    want, bound = oracle.linear_int8(host(x), w.cpu().numpy(), ws.cpu().numpy(), None, before, False, dtype)
+    near(out, want, bound)
+    assert bool((ow[:, :3] == 5).all()) and bool((ow[:, 3 + N:] == 5).all())
+
+
+@pytest.mark.parametrize("tokens", [4, 100])
+def test_linear_special_rows(tokens):
+    rng = np.random.default_rng(9)
+    x = rng.standard_normal((tokens, 300)).astype(np.float32)
+    x[0], x[1, 7], x[2, 299] = 0.0, np.nan, np.inf
+    w, ws = weights(rng, 90, 300)
+    bias = rng.standard_normal(90).astype(np.float32)
+    got = ops.linear_int8(dev(x), w, ws, dev(bias))
+    want, bound = oracle.linear_int8(x, w.cpu().numpy(), ws.cpu().numpy(), bias)
+    assert np.isnan(want[1]).all() and np.isnan(want[2]).all() and not np.isnan(want[3]).any()
+    near(got, want, bound)
+
+
+def test_linear_largest_depth():
+    """The longest reduction, every code at its largest: the sum is 131072 * 127 * 127, just inside 32 bits."""
+    K = 131072
+    x = torch.ones(3, K, device="cuda")
+    x[1] = -1.0
+    x[2, ::2] = -1.0
+    codes, ws = torch.full((2, K), 127, dtype=torch.int8, device="cuda"), torch.ones(2, device="cuda")
+    got = ops.linear_int8(x, codes, ws).cpu().numpy()
+    s = float(np.float32(1.0) / np.float32(127))
+    want = np.array([[K * 127.0 * 127.0 * s] * 2, [-K * 127.0 * 127.0 * s] * 2, [0.0, 0.0]])
+    assert np.abs(got - want).max() <= 8 * 2.0 ** -24 * K * 127
+
+
+def test_linear_nothing_to_do():
+    w, ws = weights(np.random.default_rng(0), 8, 32)
+    assert ops.linear_int8(torch.empty(0, 32, device="cuda"), w, ws).shape == (0, 8)
+
+
+# ---- rotary positions -------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("tokens,heads,width,dim", [(1, 1, 2, 2), (3, 2, 64, 64), (65, 12, 64, 32), (7, 5, 80, 40), (130, 3, 66, 50), (19, 1, 33, 6), (300, 24, 64, 64),
+                                                    (11, 2, 128, 96), (5, 2, 256, 256)])
+def test_rotary(dtype, layout, tokens, heads, width, dim):
+    rng = np.random.default_rng(tokens + width)
+    x = dev(rng.standard_normal((tokens, heads, width)).astype(np.float32), dtype)
+    f, _ = ops.rotary_frequencies(dim)
+    pos = rng.integers(-1000, 1 << 20, tokens).astype(np.int32)
+    pos[0] = (1 << 31) - 1
+    got = ops.rotary(x, dev(f), positions=dev(pos), layout=layout, factor=1.25)
+    want, bound = oracle.rotary(host(x), f, pos, layout, 1.25, dtype)
+    # (at 2^31 the angle itself, f pos, is only known to 2^-22: a step of its 64 bits times 2^31)
+    near(got, want, bound + 2.0 ** -21 * np.abs(host(x)).max() * (np.arange(tokens) == 0)[:, None, None])
+    place = x.clone()
+    assert ops.rotary(place, dev(f), positions=dev(pos), layout=layout, factor=1.25, out=place) is place
+    assert torch.equal(place, got)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("lengths", [[1], [3, 0, 5], [0, 0, 7, 1, 0], [64] * 70])
+def test_rotary_sequences(dtype, lengths):
+    """Positions by sequence; tokens in front of the first and behind the last sequence stay as they were."""
+    rng = np.random.default_rng(len(lengths))
+    n = sum(lengths)
+    cu = (2 + np.concatenate([[0], np.cumsum(lengths)])).astype(np.int32)
+    x = dev(rng.standard_normal((n + 6, 3, 64)).astype(np.float32), dtype)
+    f, _ = ops.rotary_frequencies(64)
+    out = torch.full_like(x, 9.0)
+    ops.rotary(x, dev(f), cu_seqlens=dev(cu), out=out)
+    pos = np.concatenate([np.arange(v) for v in lengths]).astype(np.int32)
+    want, bound = oracle.rotary(host(x)[2: 2 + n], f, pos, dtype=dtype)
+    near(out[2: 2 + n], want, bound)
+    assert bool((out[:2] == 9).all()) and bool((out[2 + n:] == 9).all())
+
+
+def test_rotary_views():
+    """Queries and keys inside q | k | v rows, in place; odd offsets; heads in front of tokens."""
+    rng = np.random.default_rng(3)
+    f, _ = ops.rotary_frequencies(64)
+    pos = np.arange(37, dtype=np.int32)
+    qkv = dev(rng.standard_normal((37, 9, 64)).astype(np.float32), "bf16")
+    before = qkv.clone()
+    ops.rotary(qkv[:, :6], dev(f), positions=dev(pos), out=qkv[:, :6])
+    want, bound = oracle.rotary(host(before[:, :6]), f, pos, dtype="bf16")
+    near(qkv[:, :6], want, bound)
+    assert torch.equal(qkv[:, 6:], before[:, 6:])
+    odd = dev(rng.standard_normal((37, 2 * 67 + 1)).astype(np.float32), "bf16")[:, 1:].unflatten(1, (2, 67))[..., :64]
+    want, bound = oracle.rotary(host(odd), f, pos, dtype="bf16")
+    near(ops.rotary(odd, dev(f), positions=dev(pos)), want, bound)
+    first = dev(rng.standard_normal((4, 37, 64)).astype(np.float32)).transpose(0, 1)
+    out = torch.empty(4, 37, 64, device="cuda").transpose(0, 1)
+    want, bound = oracle.rotary(host(first), f, pos)
+    near(ops.rotary(first, dev(f), positions=dev(pos), out=out), want, bound)
+
+
+def test_rotary_keeps_distances():
+    """Scores of rotated queries and keys depend on the distance alone, far into the context as at its start."""
+    rng = np.random.default_rng(4)
+    q = dev(np.repeat(rng.standard_normal((1, 1, 64)), 8, 0).astype(np.float32))
+    f, _ = ops.rotary_frequencies(64)
+    pos = np.array([0, 5, 1000, 1005, 1 << 20, (1 << 20) + 5, 1 << 30, (1 << 30) + 5], np.int32)
+    r = ops.rotary(q, dev(f), positions=dev(pos)).double().cpu().numpy()[:, 0]
+    s = (r[0::2] * r[1::2]).sum(1)
+    assert np.abs(s - s[0]).max() <= (host(q)[0] ** 2).sum() * 2.0 ** -19
+
+
+# ---- attention --------------------------------------------------------------------------------------------------
+
+def batch_of(rng, dtype, nq, nk, heads, kv_heads, width, pad=0):
+    cq, ck = (np.concatenate([[0], np.cumsum(n)]).astype(np.int32) for n in (nq, nk))
+    q = dev(rng.standard_normal((cq[-1] + pad, heads, width)).astype(np.float32), dtype)
+    k, v = (dev(rng.standard_normal((ck[-1] + pad, kv_heads, width)).astype(np.float32), dtype) for _ in range(2))
+    return q, k, v, cq, ck
+
+
+def check(dtype, q, k, v, cq, ck, max_q=None, max_k=None, **how):
+    """Against the oracle; numpy arrays among the options go to the device."""
+    t = {n: dev(x) if isinstance(x, np.ndarray) else x for n, x in how.items()}
+    left, right = t.pop("left", -1), t.pop("right", -1)
+    mq, mk = int(np.diff(cq).max()), int(np.diff(ck).max())
+    out = torch.full(q.shape, 7.0, dtype=q.dtype, device="cuda")
+    got, lse = ops.attention(q, k, v, dev(cq), max_q or mq, dev(ck), max_k or mk, window=(left, right), with_lse=True, out=out, **t)
+    want, wl, ob, lb = oracle.attention(host(q), host(k), host(v), cq, ck, dtype=dtype, **how)
+    n = cq[-1]
+    near(got[:n], want[:n], ob[:n], "out")
+    near(lse[:n], wl[:n], lb[:n], "lse")
+    assert bool((got[n:] == 7).all())
+    return got, lse
+
+
+SHAPES = [([1], [1]), ([3, 1, 2], [3, 1, 2]), ([33, 64, 7], [33, 64, 7]), ([130], [130]), ([0, 5, 0, 70], [4, 5, 0, 70]), ([1, 1, 1], [200, 3, 65]),
+          ([4, 40], [300, 100]), ([9, 2], [5, 0])]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("heads,kv_heads,width", [(2, 2, 64), (4, 1, 128), (6, 2, 40), (1, 1, 8), (3, 3, 96)])
+@pytest.mark.parametrize("nq,nk", SHAPES)
+def test_attention(dtype, heads, kv_heads, width, nq, nk):
+    rng = np.random.default_rng(sum(nq) + sum(nk) + width)
+    check(dtype, *batch_of(rng, dtype, nq, nk, heads, kv_heads, width, pad=3))
+
+
+MASKS = {
+    "causal": dict(right=0),
+    "window": dict(left=3, right=5),
+    "left": dict(left=0),
+    "far_right": dict(right=20),
+    "prefix": dict(left=4, right=0, prefix=[7, 0, 200]),
+    "documents": dict(docs=3),
+    "all": dict(left=10, right=0, prefix=[5, 1, 0], docs=2, cap=5.0, slopes=True),
+    "cap": dict(cap=3.0),
+    "slopes": dict(slopes=True),
+    "table": dict(reach=9),
+    "table_and_slopes": dict(reach=1, slopes=True, cap=20.0),
+    "hidden_by_bias": dict(reach=2, hide=True),
+    "scale": dict(scale=1.7),
+    "negative_scale": dict(scale=-0.3, cap=2.0),
+}
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("mask", MASKS)
+@pytest.mark.parametrize("heads,kv_heads,width", [(2, 2, 64), (4, 2, 128), (3, 1, 24)])
+@pytest.mark.parametrize("nq,nk", [([70, 3, 131], None), ([1, 1, 1], [90, 1, 300]), ([5, 1, 33], [90, 1, 300])])
+def test_attention_masks(dtype, mask, heads, kv_heads, width, nq, nk):
+    rng = np.random.default_rng(len(mask) + width + sum(nq))
+    nk = nk or nq
+    q, k, v, cq, ck = batch_of(rng, dtype, nq, nk, heads, kv_heads, width)
+    how = dict(MASKS[mask])
+    if how.pop("slopes", False):
+        how["slopes"] = (2.0 ** -np.arange(1, heads + 1)).astype(np.float32)
+    hide = how.pop("hide", False)
+    if "reach" in how:
+        how["bias"] = rng.standard_normal((heads, 2 * how.pop("reach") + 1)).astype(np.float32)
+        if hide:
+            how["bias"][:, :2], how["bias"][0] = -np.inf, -np.inf      # head 0 sees nothing at all
+    if "prefix" in how:
+        how["prefix"] = np.array(how["prefix"], np.int32)
+    if "docs" in how:
+        n = how.pop("docs")
+        how["doc_k"] = rng.integers(-1, n, int(ck[-1])).astype(np.int32)
+        how["doc_q"] = rng.integers(-1, n + 1, int(cq[-1])).astype(np.int32)
+    check(dtype, q, k, v, cq, ck, **how)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("first", [[0, 0, 0], [-5, 2, 400], [3, 64, 1]])
+def test_attention_first_positions(dtype, first):
+    rng = np.random.default_rng(5)
+    q, k, v, cq, ck = batch_of(rng, dtype, [1, 6, 40], [77, 130, 64], 2, 1, 64)
+    how = dict(q_first=np.array(first, np.int32), bias=rng.standard_normal((2, 65)).astype(np.float32))
+    check(dtype, q, k, v, cq, ck, **how)
+    check(dtype, q, k, v, cq, ck, left=30, right=0, **how)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("nq", [1, 3, 90])
+@pytest.mark.parametrize("width", [64, 128])
+def test_attention_long(dtype, nq, width):
+    """Long sequences, where a call of few queries is split over the keys; the maximum far back, and in the last key."""
+    rng = np.random.default_rng(nq)
+    q, k, v, cq, ck = batch_of(rng, dtype, [nq, nq], [5003, 1], 4, 2, width)
+    check(dtype, q, k, v, cq, ck)
+    k[17] *= 6.0
+    k[5002] *= 7.0
+    check(dtype, q, k, v, cq, ck, cap=30.0)
+    check(dtype, q, k, v, cq, ck, left=100, right=0, prefix=np.array([20, 0], np.int32))
+    doc = np.full(5004, -1, np.int32)
+    doc[4000:4100] = 1
+    check(dtype, q, k, v, cq, ck, doc_k=doc, doc_q=np.ones(2 * nq, np.int32))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("nq", [1, 40])
+def test_attention_unseen_keys_hold_anything(dtype, nq):
+    """NaN and infinities in keys behind the sequences' ends, between them and in documents of negative number."""
+    rng = np.random.default_rng(6)
+    q, k, v, cq, ck = batch_of(rng, dtype, [nq, nq], [200, 70], 2, 2, 64, pad=64)
+    doc = rng.integers(0, 2, int(ck[-1]) + 64).astype(np.int32)
+    doc[rng.integers(0, 270, 60)] = -1
+    doc[64:128] = -1
+    bad = torch.from_numpy(doc < 0).cuda()
+    bad[270:] = True
+    for t, x in ((k, math.nan), (v, math.inf)):
+        t[bad] = x
+    v[270] = math.nan
+    doc_q = rng.integers(0, 2, 2 * nq + 64).astype(np.int32)
+    check(dtype, q, k, v, cq, ck, doc_k=doc, doc_q=doc_q)
+    k[:, :], v[:, :] = torch.where(bad[:, None, None] & (torch.arange(len(bad), device="cuda") < 270)[:, None, None], torch.zeros_like(k), k), \
+        torch.where(bad[:, None, None] & (torch.arange(len(bad), device="cuda") < 270)[:, None, None], torch.zeros_like(v), v)
+    check(dtype, q, k, v, cq, ck)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_attention_extreme_scores(dtype):
+    """Scores so far apart that one key takes all, and scores near the lowest value of the type."""
+    rng = np.random.default_rng(7)
+    q, k, v, cq, ck = batch_of(rng, dtype, [50], [50], 2, 2, 64)
+    got, _ = check(dtype, q * 60, k, v, cq, ck)
+    low = np.full((2, 3), -3.0e38, np.float32)
+    out = ops.attention(q, k, v, dev(cq), 50, bias=dev(low))
+    assert bool(torch.isfinite(out).all())                  # (adding anything to -3e38 is lost: all keys weigh the same)
+    near(out[:, 0], host(v)[:, 0].astype(np.float64).mean(0)[None].repeat(50, 0), np.full((50, 64), 2.0 ** -7 * np.abs(host(v)).max()))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_attention_views(dtype):
+    """q, k and v inside one buffer of q | k | v rows; heads in front of tokens; the output inside a wider one."""
+    rng = np.random.default_rng(8)
+    n, A = 100, 4
+    cu = np.array([0, 60, 100], np.int32)
+    qkv = dev(rng.standard_normal((n, 3 * A, 64)).astype(np.float32), dtype)
+    q, k, v = qkv[:, :A], qkv[:, A: 2 * A], qkv[:, 2 * A:]
+    wide = torch.full((n, A + 2, 64), 3.0, dtype=TYPES[dtype], device="cuda")
+    ops.attention(q, k, v, dev(cu), 60, out=wide[:, 1: 1 + A])
+    want, _, ob, _ = oracle.attention(host(q), host(k), host(v), cu, cu, dtype=dtype)
+    near(wide[:, 1: 1 + A], want, ob)
+    assert bool((wide[:, 0] == 3).all()) and bool((wide[:, A + 1] == 3).all())
+    t = [x.transpose(0, 1).contiguous().transpose(0, 1) for x in (q, k, v)]
+    near(ops.attention(*t, dev(cu), 60), want, ob)
+
+
+def test_attention_bounds_larger_than_the_lengths():
+    rng = np.random.default_rng(10)
+    q, k, v, cq, ck = batch_of(rng, "bf16", [1, 1], [300, 40], 4, 1, 64)
+    check("bf16", q, k, v, cq, ck, max_q=1, max_k=9000)
+    q, k, v, cq, ck = batch_of(rng, "bf16", [30, 50], [30, 50], 4, 1, 64)
+    check("bf16", q, k, v, cq, ck, max_q=500, max_k=70000)
+
+
+def test_attention_nothing_to_do():
+    e = torch.empty(0, 2, 64, device="cuda")
+    cu = torch.zeros(3, dtype=torch.int32, device="cuda")
+    assert ops.attention(e, e, e, cu, 0).shape == (0, 2, 64)
+    q = torch.ones(4, 2, 64, device="cuda")
+    out, lse = ops.attention(q, e, e, dev(np.array([0, 4], np.int32)), 4, cu[:2], 0, with_lse=True)
+    assert bool((out == 0).all()) and bool((lse == -math.inf).all())
+
+
+def test_attention_inconsistent_offsets_stay_inside():
+    """Offsets that point outside, fall, or exceed the bounds: clamped, nothing else is promised."""
+    rng = np.random.default_rng(11)
+    q, k, v, *_ = batch_of(rng, "bf16", [64], [64], 2, 2, 64)
+    for cu in ([0, 1 << 30], [-5, 64], [64, 0], [10, 5], [0, 64]):
+        ops.attention(q, k, v, dev(np.array(cu, np.int32)), 30)
+        ops.attention(q[:1].contiguous(), k, v, dev(np.array([0, 1], np.int32)), 1, dev(np.array(cu, np.int32)), 64)
+    torch.cuda.synchronize()
+
+
+# ---- together ---------------------------------------------------------------------------------------------------
+
+def block(x, w, freq, cu, most, heads):
+    """An attention block as a layer uses the operators: q | k | v, rotary on q and k, attention, output and residual."""
+    qkv = ops.linear_int8(x, w["qkv"], w["qkv_s"], w["qkv_b"]).view(len(x), 3 * heads, -1)
+    ops.rotary(qkv[:, : 2 * heads], freq, cu_seqlens=cu, out=qkv[:, : 2 * heads])
+    att = ops.attention(qkv[:, :heads], qkv[:, heads: 2 * heads], qkv[:, 2 * heads:], cu, most, cap=30.0, window=(16, 16), bias=w["bias"])
+    return ops.linear_int8(att.view(len(x), -1), w["o"], w["o_s"], w["o_b"], residual=x)
+
+
+def block_inputs(dtype, lengths, heads=4):
+    rng = np.random.default_rng(12)
+    H, n = heads * 64, sum(lengths)
+    w = {}
+    for name, cols in (("qkv", 3 * H), ("o", H)):
+        w[name], w[name + "_s"] = weights(rng, cols, H)
+        w[name + "_b"] = dev(rng.standard_normal(cols).astype(np.float32) * 0.1)
+    w["bias"] = dev(rng.standard_normal((heads, 17)).astype(np.float32))
+    cu = np.concatenate([[0], np.cumsum(lengths)]).astype(np.int32)
+    return dev(rng.standard_normal((n, H)).astype(np.float32), dtype), w, dev(ops.rotary_frequencies(64)[0]), cu
+
+
+def test_block():
+    """In fp32: the chain of oracles, whose codes agree but where an input to the second product lies within rounding of a half."""
+    heads, lengths = 4, [5, 1, 90, 33]
+    x, w, freq, cu = block_inputs("fp32", lengths, heads)
+    got = block(x, w, freq, dev(cu), 90, heads).double().cpu().numpy()
+    n = len(x)
+    h = {k: v.cpu().numpy() for k, v in w.items()}
+    qkv = oracle.linear_int8(host(x), h["qkv"], h["qkv_s"], h["qkv_b"])[0].reshape(n, 3 * heads, 64)
+    pos = np.concatenate([np.arange(v) for v in lengths])
+    qk = oracle.rotary(qkv[:, : 2 * heads], freq.cpu().numpy(), pos)[0]
+    att = oracle.attention(qk[:, :heads], qk[:, heads:], qkv[:, 2 * heads:], cu, cu, cap=30.0, left=16, right=16, bias=h["bias"])[0]
+    want, bound = oracle.linear_int8(att.reshape(n, -1), h["o"], h["o_s"], h["o_b"], host(x))
+    # one code of a row off by one: a step of its scale times the largest weight
+    step = np.abs(att.reshape(n, -1)).max(1, keepdims=True) / 127 * np.abs(h["o"]).max(1)[None] * h["o_s"][None]
+    off = np.abs(got - want)
+    assert (off <= bound + 1e-5 + step).all()
+    assert (off <= bound + 1e-5).mean() > 0.9
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_block_in_a_graph(dtype):
+    """Captured once, replayed on new inputs with eager work in between: the same bits as eager calls."""
+    lengths = [200, 64, 1, 700]
+    x, w, freq, cu = block_inputs(dtype, lengths)
+    cu = dev(cu)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        block(x, w, freq, cu, 700, 4)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = block(x, w, freq, cu, 700, 4)
+    for i in range(3):
+        x.copy_(torch.randn(x.shape, generator=torch.Generator("cuda").manual_seed(i), device="cuda"))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = y.clone()
+        assert torch.equal(got, block(x, w, freq, cu, 700, 4))
+
+
+def test_few_rows_in_two_graphs():
+    """Split calls captured twice have a workspace each: replayed at the same time, both are right."""
+    rng = np.random.default_rng(13)
+    q, k, v, cq, ck = batch_of(rng, "bf16", [1, 1], [5000, 3000], 4, 2, 64)
+    w, ws = weights(rng, 300, 500)
+    x = dev(rng.standard_normal((3, 500)).astype(np.float32))
+    args = (dev(cq), 1, dev(ck), 5000)
+    want = ops.attention(q, k, v, *args), ops.linear_int8(x, w, ws)
+    graphs, outs = [], []
+    for _ in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append((ops.attention(q, k, v, *args), ops.linear_int8(x, w, ws)))
+        graphs.append(g)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(5):
+        for g, s in zip(graphs, streams):
+            s.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(s):
+                g.replay()
+        torch.cuda.synchronize()
+        for o in outs:
+            assert torch.equal(o[0], want[0]) and torch.equal(o[1], want[1])
+            o[0].zero_(), o[1].zero_()
+
+
+def test_another_stream():
+    rng = np.random.default_rng(14)
+    q, k, v, cq, ck = batch_of(rng, "bf16", [1, 1], [5000, 3000], 4, 2, 64)
+    want = ops.attention(q, k, v, dev(cq), 1, dev(ck), 5000)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        got = [ops.attention(q, k, v, dev(cq), 1, dev(ck), 5000) for _ in range(4)]
+    s.synchronize()
+    assert all(torch.equal(g, want) for g in got)
+
+
+# ---- refusals ---------------------------------------------------------------------------------------------------
+
+def test_refusals():
+    x = torch.ones(4, 32, device="cuda")
+    w, ws = weights(np.random.default_rng(0), 8, 32)
+    w1, ws1 = weights(np.random.default_rng(0), 8, 33)
+    q = torch.ones(4, 2, 64, device="cuda")
+    cu = dev(np.array([0, 4], np.int32))
+    f = dev(ops.rotary_frequencies(64)[0])
+    pos = torch.arange(4, dtype=torch.int32, device="cuda")
+    bad = [
+        lambda: ops.linear_int8(x.half(), w, ws),
+        lambda: ops.linear_int8(x, w.float(), ws),
+        lambda: ops.linear_int8(x, w1, ws1),
+        lambda: ops.linear_int8(x.t(), w[:, :4], ws),
+        lambda: ops.linear_int8(x, w, ws[:7]),
+        lambda: ops.linear_int8(x, w, ws.double()),
+        lambda: ops.linear_int8(x, w, ws, gelu=True, residual=torch.ones(4, 8, device="cuda")),
+        lambda: ops.linear_int8(x, w, ws, residual=torch.ones(4, 8, device="cuda").bfloat16()),
+        lambda: ops.linear_int8(x, w, ws, out=torch.ones(5, 8, device="cuda")),
+        lambda: ops.linear_int8(x, w.flatten()[1:].as_strided((7, 32), (32, 1)), ws[:7]),
+        lambda: ops.linear_int8(x, torch.ones(8, 33, dtype=torch.int8, device="cuda")[:, :32], ws),
+        lambda: ops.linear_int8(x, w.cpu(), ws),
+        lambda: ops.linear_int8(x.clone().requires_grad_(), w, ws),
+        lambda: ops.rotary(q, f),
+        lambda: ops.rotary(q, f, positions=pos, cu_seqlens=cu),
+        lambda: ops.rotary(q, f.float(), positions=pos),
+        lambda: ops.rotary(q, f, positions=pos[:3]),
+        lambda: ops.rotary(q, f, positions=pos.long()),
+        lambda: ops.rotary(q, f, positions=pos, layout="other"),
+        lambda: ops.rotary(q[..., ::2], f, positions=pos),
+        lambda: ops.rotary(q[..., :32].contiguous(), f, positions=pos),
+        lambda: ops.rotary(q, f, positions=pos, out=torch.ones(4, 1, 64, device="cuda").expand(4, 2, 64)),
+        lambda: ops.attention(q, q, q, cu.long(), 4),
+        lambda: ops.attention(q, q[:3], q[:3], cu, 4),
+        lambda: ops.attention(q, q.bfloat16(), q.bfloat16(), cu, 4),
+        lambda: ops.attention(q, q[:, :1], q[:, :1, :32], cu, 4),
+        lambda: ops.attention(torch.ones(4, 3, 64, device="cuda"), q, q, cu, 4, cu, 4),
+        lambda: ops.attention(*[torch.ones(4, 2, 136, device="cuda")] * 3, cu, 4),
+        lambda: ops.attention(*[torch.ones(4, 2, 20, device="cuda")] * 3, cu, 4),
+        lambda: ops.attention(*[torch.ones(4, 2, 66, device="cuda")[..., :64]] * 3, cu, 4),
+        lambda: ops.attention(q, q, q, cu, 4, causal=True, window=(-1, 3)),
+        lambda: ops.attention(q, q, q, cu, 4, doc_k=pos),
+        lambda: ops.attention(q, q, q, cu, 4, bias=torch.ones(2, 4, device="cuda")),
+        lambda: ops.attention(q, q, q, cu, 4, slopes=torch.ones(3, device="cuda")),
+        lambda: ops.attention(q, q, q, cu, 4, out=q),
+        lambda: ops.attention(q, q, q, cu, 4, scale=math.inf),
+        lambda: ops.attention(q, q, q, cu, -1),
+    ]
+    for i, call in enumerate(bad):
+        with pytest.raises((ValueError, sp.SpError)):
+            call()
+            raise AssertionError(f"call {i} was taken")
+    with torch.no_grad():
+        ops.linear_int8(x.clone().requires_grad_(), w, ws)
