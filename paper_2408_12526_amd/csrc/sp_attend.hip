@@ -1,4 +1,17 @@
 // Attention over packed sequences with capped scores, a bias by distance and masks (the definition is in sp_ops.h).
+//
+// One pass over the keys with the running maximum and sum of the softmax, products on the matrix cores.  The rows of a tile are (query, query
+// head) pairs of one key head, r = query * share + head % share, so that heads that share keys share their tiles.  A wave takes 32 rows;
+// per block of 32 keys:
+//   S^T = K Q^T      (A operand: key rows from LDS; B operand: the rows' queries, in registers throughout)
+//   scores           cap, slopes, table, mask: a row is a lane column, its keys sit in the registers of lanes l and l + 32; what a tile
+//                    does not need (a mask where every row sees it all, the table where all distances are beyond its reach) is
+//                    skipped by uniform branches
+//   O^T += V^T P^T   (bf16: value fragments come transposed out of LDS by the transposing read; fp32: one value a lane)
+// in two shapes: many rows, four waves with 32 rows each on the same key tiles; and few rows (up to 32 a sequence and key head, as one
+// query against a long sequence), four waves with the same rows on key tiles of their own, joined at the end.  Either can be split over the
+// keys where there are few workgroups; a small launch joins the parts.
+#include <atomic>
 #include <cmath>
 
 #include "sp_ops_internal.h"
@@ -7,73 +20,623 @@ namespace sp {
 
 namespace {
 
-// A wave takes one query of one head: a lane a key for the scores, a lane two dimensions for the values.
-template <class E>
-__global__ __launch_bounds__(256) void attend_simple_kernel(sp_attention_args p)
+constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.69314718055994531f;
+constexpr int kWaveRows = 32, kManyRows = 128;
+constexpr int kTablePad = 96;           // entries on each side of the table in LDS: a wave's 32 rows and a tile's 64 keys are less than that apart
+constexpr int kTableBytes = 14336;      // largest table in LDS
+
+struct AttendArgs {
+    const char *q, *k, *v;
+    char* out;
+    float* lse;
+    size_t qt, qh, kt, kh, vt, vh, ot, oh;                  // strides in bytes
+    const int32_t *cu_q, *cu_k, *prefix, *q_first, *doc_q, *doc_k;
+    const float *slopes, *bias;
+    float *part, *part_ml;                                  // [splits][total_q * heads][DP] sums, and (maximum, sum) pairs
+    float scale, cap;
+    int batch, heads, kv_heads, share, width, total_q, total_k, max_q, max_k, left, right, reach;
+    int items, splits, table;                               // table: whether the bias is in LDS
+};
+
+__device__ __forceinline__ void sequence_range(int t0, int t1, int total, int most, int& at, int& n)
 {
-    const int lane = threadIdx.x & 63, h = blockIdx.y, b = blockIdx.z;
-    const int r = blockIdx.x * 4 + (threadIdx.x >> 6);
-    auto range = [](const int32_t* cu, int b, int total, int most, int& t0, int& n) {
-        t0 = cu[b];
-        t0 = t0 < 0 ? 0 : t0 > total ? total : t0;
-        n = cu[b + 1] - t0;
-        n = n < 0 ? 0 : n > most ? most : n;
-        n = n > total - t0 ? total - t0 : n;
-    };
-    int q0, nq, k0, nk;
-    range(p.cu_q, b, p.total_q, p.max_q, q0, nq);
-    range(p.cu_k, b, p.total_k, p.max_k, k0, nk);
-    if (r >= nq) return;
-    const int i = (p.q_first ? p.q_first[b] : nk - nq) + r, t = q0 + r, hk = h / (p.heads / p.kv_heads);
-    const E* q = (const E*)p.q + t * p.q_token + h * p.q_head;
-    const int doc = p.doc_q ? p.doc_q[t] : 0, prefix = p.prefix ? p.prefix[b] : 0;
-    float m = -INFINITY, l = 0.f, o0 = 0.f, o1 = 0.f;
-    for (int j0 = 0; j0 < nk; j0 += 64) {
-        const int j = j0 + lane, d = j - i;
-        bool seen = j < nk && (((p.left < 0 || d >= -p.left) && (p.right < 0 || d <= p.right)) || j < prefix);
-        if (seen && p.doc_k) { const int dk = p.doc_k[k0 + j]; seen = dk == doc && dk >= 0; }
-        float s = -INFINITY;
-        if (seen) {
-            const E* k = (const E*)p.k + (k0 + j) * p.k_token + hk * p.k_head;
-            s = 0.f;
-            for (int e = 0; e < p.width; ++e) s = __builtin_fmaf((float)q[e], (float)k[e], s);
-            s *= p.scale;
-            if (p.cap > 0.f) s = p.cap * tanhf(s / p.cap);
-            if (p.slopes) s -= p.slopes[h] * fabsf((float)d);
-            if (p.bias) s += p.bias[(size_t)h * (2 * p.reach + 1) + (d < -p.reach ? -p.reach : d > p.reach ? p.reach : d) + p.reach];
+    at = t0 < 0 ? 0 : t0 > total ? total : t0;
+    n = t1 - at;
+    n = n < 0 ? 0 : n > most ? most : n;
+    n = n > total - at ? total - at : n;
+}
+
+// A bias in units of the base-2 logarithm; finite ones stay finite.
+__device__ __forceinline__ float in_log2(float b) { return __builtin_isinf(b) ? b : __builtin_amdgcn_fmed3f(b * kLog2e, -3.0e38f, 3.0e38f); }
+
+template <class E>
+__device__ __forceinline__ float capped(float s, float cap, float inv_cap)
+{
+    if (sizeof(E) == 4) return cap * tanhf(s * inv_cap);
+    // tanh(y) = 1 - 2 / (e^(2 y) + 1): 2^-23 off in absolute value, far inside what bf16 operands leave of a score
+    return __builtin_fmaf(-2.f * cap, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(s * (2.f * kLog2e * inv_cap)) + 1.f), cap);
+}
+
+template <class E, int DP, bool FEW>
+struct Shape {
+    static constexpr bool B16 = sizeof(E) == 2;
+    static constexpr int KT = FEW || !B16 ? 32 : 64;        // keys of a tile
+    static constexpr int NT = FEW ? 64 : 256;               // threads that fetch it
+    static constexpr int RC = DP * (int)sizeof(E) / 16;     // 16-byte chunks of a row
+    static constexpr int LPT = KT * RC / NT, RS = NT / RC;  // chunks a thread fetches, rows between them
+    static constexpr int TILE = KT * RC * 16;               // bytes
+    static constexpr int BUFS = FEW ? 4 : 2;                // FEW: one of each wave
+    static constexpr int DOCS = BUFS * 2 * TILE, TABLE = DOCS + BUFS * KT * 4;      // offsets in LDS
+    static constexpr int JOIN = DOCS;                       // (FEW: maxima and sums of the waves, over the documents)
+    static constexpr size_t LDS = TABLE + (FEW ? 1024 - BUFS * KT * 4 : 0);
+    static_assert(BUFS * 2 * TILE >= 4 * kWaveRows * DP * (FEW ? 4 : (int)sizeof(E)), "the outputs reuse the tiles");
+    // Chunk c of row r is in slot c ^ swizzle(r): the sixteen rows that a quarter of a read takes, or the four rows by four chunks of a
+    // transposing one, lie in different banks.
+    static __device__ __forceinline__ int key_slot(int r, int c) { return r * RC + (c ^ (RC == 8 ? (r >> 1) & 7 : r & 15)); }
+    static __device__ __forceinline__ int value_slot(int r, int c)
+    {
+        return r * RC + (c ^ (!B16 ? (r >> 2 & 1) << 3 : RC == 8 ? (r >> 1 & 1) << 2 : (r & 3) << 2));
+    }
+};
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+template <class E, int DP, bool FEW>
+__global__ __launch_bounds__(256, FEW ? (sizeof(E) == 4 && DP == 128 ? 1 : 2) : (DP == 64 && sizeof(E) == 2 ? 3 : 2)) void attend_kernel(AttendArgs p)
+{
+    using S = Shape<E, DP, FEW>;
+    constexpr int KT = S::KT, NB = KT / 32, RC = S::RC, LPT = S::LPT, RS = S::RS, ND = DP / 32;
+    extern __shared__ char lds[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), j31 = lane & 31, g = lane >> 5;
+
+    // ---- which rows ----
+    int b, hk, r0, split, q0, nq, c0, c1;
+    if (FEW) {
+        b = blockIdx.x;
+        hk = blockIdx.y;
+        split = blockIdx.z;
+        r0 = 0;
+        c0 = p.cu_q[b];
+        c1 = p.cu_q[b + 1];
+    } else {
+        // Neighbouring items of one key head read the same keys: contiguous runs per XCD (workgroup id mod 8).
+        const int total = p.items * p.kv_heads * p.splits, chunk = (total + 7) >> 3;
+        const int lin = (int)(blockIdx.x & 7) * chunk + (int)(blockIdx.x >> 3);
+        if ((int)(blockIdx.x >> 3) >= chunk || lin >= total) return;
+        split = lin % p.splits;
+        const int item = lin / p.splits % p.items;
+        hk = lin / p.splits / p.items;
+        // Item i belongs to the last sequence with cu * share / 128 + b <= i: every sequence gets as many as it has blocks of rows, at least
+        b = last_sequence(p.cu_q, p.batch, lane, [&](int i, int c) { return ((int64_t)c * p.share >> 7) + i <= item; }, c0, c1);
+        const int64_t start = (int64_t)item - (((int64_t)c0 * p.share >> 7) + b);
+        if (start < 0 || start > (1 << 23)) return;
+        r0 = (int)start * kManyRows;
+    }
+    sequence_range(c0, c1, p.total_q, p.max_q, q0, nq);
+    const int rows = nq * p.share;
+    if (r0 >= rows) return;                                 // (the whole workgroup)
+    int k0, n;
+    sequence_range(p.cu_k[b], p.cu_k[b + 1], p.total_k, p.max_k, k0, n);
+    int first = p.q_first ? p.q_first[b] : n - nq;
+    first = first < -(1 << 30) ? -(1 << 30) : first > 1 << 30 ? 1 << 30 : first;
+    int prefix = p.prefix ? p.prefix[b] : 0;
+    prefix = prefix < 0 ? 0 : prefix > n ? n : prefix;
+
+    const int rw = r0 + (FEW ? 0 : wave * kWaveRows);       // the wave's first row
+    const bool idle = rw >= rows;
+    const int r = rw + j31, rv = r < rows ? r : rows - 1, query = rv / p.share, head = hk * p.share + rv - query * p.share;
+    const int pos = first + query;
+    auto first_seen = [&](int i) { const int64_t x = p.left < 0 ? 0 : (int64_t)i - p.left; return (int)(x < 0 ? 0 : x > n ? n : x); };
+    auto last_seen = [&](int i) { const int64_t x = p.right < 0 ? n - 1 : (int64_t)i + p.right; return (int)(x < -1 ? -1 : x > n - 1 ? n - 1 : x); };
+    const int lo = first_seen(pos), hi = last_seen(pos);
+    // of the wave: positions, and the keys that any and that every row sees
+    const int rl = rw + kWaveRows - 1 < rows ? rw + kWaveRows - 1 : rows - 1;
+    const int pos_a = first + (idle ? 0 : rw / p.share), pos_z = first + rl / p.share;
+    const int any_lo = first_seen(pos_a), any_hi = last_seen(pos_z), all_lo = first_seen(pos_z), all_hi = last_seen(pos_a);
+
+    // ---- which key tiles: those of the prefix, then those of the window of all the workgroup's rows ----
+    const int re = r0 + (FEW ? kWaveRows : kManyRows) - 1 < rows ? r0 + (FEW ? kWaveRows : kManyRows) - 1 : rows - 1;
+    const int w_lo = first_seen(first + r0 / p.share), w_hi = last_seen(first + re / p.share);
+    const int tiles1 = (prefix + KT - 1) / KT, from2 = w_lo / KT > tiles1 ? w_lo / KT : tiles1, to2 = (w_hi + KT) / KT;     // (w_hi >= -1)
+    const int tiles = tiles1 + (w_hi >= w_lo && to2 > from2 ? to2 - from2 : 0);
+    const int per = (tiles + p.splits - 1) / p.splits, t_a = split * per, t_z = t_a + per < tiles ? t_a + per : tiles;
+    auto tile_start = [&](int t) { return (t < tiles1 ? t : t - tiles1 + from2) * KT; };
+
+    // ---- queries, table ----
+    const char* qrow = p.q + (size_t)(q0 + query) * p.qt + (size_t)head * p.qh;
+    constexpr int QF = S::B16 ? DP / 16 : DP / 8;
+    u32x4 qf[QF];                                           // bf16: dimensions 16 s + 8 g ..; fp32: 8 s + 4 g ..
+#pragma unroll
+    for (int s = 0; s < QF; ++s) {
+        const int byte = (2 * s + g) * 16;
+        qf[s] = byte < p.width * (int)sizeof(E) ? *(const u32x4*)(qrow + byte) : u32x4{0, 0, 0, 0};
+    }
+    const int doc = p.doc_q ? p.doc_q[q0 + query] : 0;
+    const float slope = p.slopes ? p.slopes[head] * kLog2e : 0.f;
+    const float* brow = p.bias ? p.bias + (size_t)head * (2 * p.reach + 1) : nullptr;
+    const float bias_left = brow ? in_log2(brow[0]) : 0.f, bias_right = brow ? in_log2(brow[2 * p.reach]) : 0.f;
+    float* table = (float*)(lds + S::TABLE);
+    const int pitch = 2 * (p.reach + kTablePad) + 1;
+    if (!FEW && p.table) {
+        for (int h = 0; h < p.share; ++h)
+            for (int e = tid; e < pitch; e += 256) {
+                int d = e - kTablePad;
+                d = d < 0 ? 0 : d > 2 * p.reach ? 2 * p.reach : d;
+                table[h * pitch + e] = in_log2(p.bias[(size_t)(hk * p.share + h) * (2 * p.reach + 1) + d]);
+            }
+        barrier_lds();
+    }
+    const float* tab = table + (head - hk * p.share) * pitch + p.reach + kTablePad;
+
+    // ---- documents of the workgroup's rows ----
+    int doc_lo = 0x7fffffff, doc_hi = -1;
+    bool doc_one = true;                                    // all rows have the same one
+    if (p.doc_q && !FEW) {
+        for (int x = r0 / p.share + lane; x <= re / p.share; x += 64) {
+            const int d = p.doc_q[q0 + x];
+            if (d >= 0) {
+                doc_lo = d < doc_lo ? d : doc_lo;
+                doc_hi = d > doc_hi ? d : doc_hi;
+            } else {
+                doc_one = false;
+            }
         }
-        const float mn = fmaxf(m, wave_max(s));
-        if (mn == -INFINITY) continue;
-        const float al = expf(m - mn), e = expf(s - mn);
-        l = l * al + wave_sum(e);
-        o0 *= al;
-        o1 *= al;
-        m = mn;
-        for (int c = 0; c < 64 && j0 + c < nk; ++c) {
-            const float w = __shfl(e, c);
-            if (w == 0.f) continue;
-            const E* v = (const E*)p.v + (k0 + j0 + c) * p.v_token + hk * p.v_head;
-            if (lane < p.width) o0 += w * (float)v[lane];
-            if (lane + 64 < p.width) o1 += w * (float)v[lane + 64];
+#pragma unroll
+        for (int x = 1; x < 64; x <<= 1) {
+            const int l = __shfl_xor(doc_lo, x), h = __shfl_xor(doc_hi, x);
+            doc_lo = l < doc_lo ? l : doc_lo;
+            doc_hi = h > doc_hi ? h : doc_hi;
+        }
+        doc_one = __all(doc_one) && doc_lo == doc_hi;
+    }
+
+    // ---- fetching: thread -> chunk fc of rows fr + i RS ----
+    const int ft = FEW ? lane : tid, fc = ft % RC, fr = ft / RC;
+    const bool inside = fc * 16 < p.width * (int)sizeof(E);
+    const char* kbase = p.k + (size_t)k0 * p.kt + (size_t)hk * p.kh + fc * 16;
+    const char* vbase = p.v + (size_t)k0 * p.vt + (size_t)hk * p.vh + fc * 16;
+    u32x4 kr[LPT], vr[LPT];
+    int dr[LPT], dk = 0;                                    // documents of the fetched rows; of the tile's key `ft`
+    auto fetch = [&](int j0) {
+#pragma unroll
+        for (int i = 0; i < LPT; ++i) {
+            int j = j0 + fr + i * RS;
+            j = j < n ? j : n - 1;
+            if (inside) {
+                kr[i] = *(const u32x4*)(kbase + (size_t)(unsigned)j * (unsigned)p.kt);
+                vr[i] = *(const u32x4*)(vbase + (size_t)(unsigned)j * (unsigned)p.vt);
+            }
+            if (p.doc_k) dr[i] = p.doc_k[k0 + j];
+        }
+        if (p.doc_k && ft < KT) dk = p.doc_k[k0 + (j0 + ft < n ? j0 + ft : n - 1)];
+    };
+    char* const mine = lds + (FEW ? wave * 2 * S::TILE : 0);
+    auto put = [&](int j0, int buf) {
+        char* to = mine + (FEW ? 0 : buf * 2 * S::TILE);
+#pragma unroll
+        for (int i = 0; i < LPT; ++i) {
+            const int row = fr + i * RS;
+            // (values that no row sees become zeros: a weight of zero does not hide a NaN)
+            const bool seen = inside && j0 + row < n && !(p.doc_k && dr[i] < 0);
+            *(u32x4*)(to + S::key_slot(row, fc) * 16) = inside ? kr[i] : u32x4{0, 0, 0, 0};
+            *(u32x4*)(to + S::TILE + S::value_slot(row, fc) * 16) = seen ? vr[i] : u32x4{0, 0, 0, 0};
+        }
+        if (p.doc_k && ft < KT) ((int*)(lds + S::DOCS))[(FEW ? wave : buf) * KT + ft] = dk;
+    };
+
+    // ---- one tile ----
+    f32x16 o[ND];
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
+    float mrun = -INFINITY, lrun = 0.f;                     // (of this half's keys)
+    const bool raw = !(p.cap > 0.f) && !p.slopes && !p.bias && p.scale > 0.f;
+    const float mult = raw ? p.scale * kLog2e : 1.f, pre = p.cap > 0.f ? p.scale : p.scale * kLog2e, inv_cap = p.cap > 0.f ? 1.f / p.cap : 0.f;
+    auto compute = [&](int j0, int buf, bool doc_mask) {
+        const bool in_prefix = j0 < prefix;
+        if (!in_prefix && (j0 > any_hi || j0 + KT <= any_lo)) return;       // (the wave sees none of it)
+        const char* kt = mine + (FEW ? 0 : buf * 2 * S::TILE);
+        const char* vt = kt + S::TILE;
+        f32x16 sc[NB];
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) sc[nb][e] = 0.f;
+            const int row = nb * 32 + j31;
+#pragma unroll
+            for (int s = 0; s < QF; ++s) {
+                const u32x4 a = *(const u32x4*)(kt + S::key_slot(row, 2 * s + g) * 16);
+                if constexpr (S::B16) {
+                    sc[nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, qf[s]), sc[nb], 0, 0, 0);
+                } else {
+                    const f32x4 fa = __builtin_bit_cast(f32x4, a), fq = __builtin_bit_cast(f32x4, qf[s]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sc[nb] = __builtin_amdgcn_mfma_f32_32x32x2f32(fa[e], fq[e], sc[nb], 0, 0, 0);
+                }
+            }
+        }
+        // Register v of block nb is key j0 + 32 nb + 8 (v / 4) + 4 g + v % 4.
+#define EACH_SCORE for (int nb = 0; nb < NB; ++nb) _Pragma("unroll") for (int v = 0; v < 16; ++v)
+#define KEY_OFFSET (32 * nb + 8 * (v >> 2) + (v & 3))
+        const int jg = j0 + 4 * g;
+        if (!raw) {
+#pragma unroll
+            EACH_SCORE sc[nb][v] *= pre;
+            if (p.cap > 0.f) {
+#pragma unroll
+                EACH_SCORE sc[nb][v] = capped<E>(sc[nb][v], p.cap, inv_cap) * kLog2e;
+            }
+            if (p.slopes) {
+                const float d0 = (float)(jg - pos);
+#pragma unroll
+                EACH_SCORE sc[nb][v] = __builtin_fmaf(-slope, __builtin_fabsf(d0 + (float)KEY_OFFSET), sc[nb][v]);
+            }
+            if (p.bias) {
+                if (j0 - pos_z >= p.reach) {
+#pragma unroll
+                    EACH_SCORE sc[nb][v] += bias_right;
+                } else if (j0 + KT - 1 - pos_a <= -p.reach) {
+#pragma unroll
+                    EACH_SCORE sc[nb][v] += bias_left;
+                } else if (!FEW && p.table) {
+                    const float* at = tab + (jg - pos);
+#pragma unroll
+                    EACH_SCORE sc[nb][v] += at[KEY_OFFSET];
+                } else {
+#pragma unroll
+                    EACH_SCORE {
+                        int d = jg + KEY_OFFSET - pos;
+                        d = d < -p.reach ? -p.reach : d > p.reach ? p.reach : d;
+                        sc[nb][v] += in_log2(brow[d + p.reach]);
+                    }
+                }
+            }
+        }
+        if (!(j0 + KT <= prefix || (j0 >= all_lo && j0 + KT - 1 <= all_hi))) {
+            const int a = lo - jg, z = hi - jg, pr = prefix - jg;
+#pragma unroll
+            EACH_SCORE if (!((KEY_OFFSET >= a && KEY_OFFSET <= z) || KEY_OFFSET < pr)) sc[nb][v] = -INFINITY;
+        }
+        if (doc_mask) {
+            const int* dt = (const int*)(lds + S::DOCS) + (FEW ? wave : buf) * KT + 4 * g;
+#pragma unroll
+            EACH_SCORE { const int x = dt[KEY_OFFSET]; if (x != doc || x < 0) sc[nb][v] = -INFINITY; }
+        }
+        float mx = sc[0][0];
+#pragma unroll
+        EACH_SCORE mx = __builtin_fmaxf(mx, sc[nb][v]);
+        {
+            float l = mx, h = mx;
+            swap_halves(l, h);
+            mx = __builtin_fmaxf(l, h);
+        }
+        if (__any(mx > mrun)) {
+            mx = __builtin_fmaxf(mx, mrun);
+            const float alpha = mrun == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mrun - mx) * mult);
+            mrun = mx;
+            lrun *= alpha;
+#pragma unroll
+            for (int d = 0; d < ND; ++d)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[d][e] *= alpha;
+        }
+        const float nm = mrun == -INFINITY ? 0.f : -mrun * mult;    // (a row that has seen nothing yet: weights 2^-inf)
+        float psum = 0.f;
+#pragma unroll
+        EACH_SCORE {
+            const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[nb][v], mult, nm));
+            psum += e;
+            sc[nb][v] = e;
+        }
+        lrun += psum;
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            if constexpr (S::B16) {
+#pragma unroll
+                for (int s2 = 0; s2 < 2; ++s2) {
+                    bf16x8 pf;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) pf[e] = (bf16)sc[nb][8 * s2 + e];
+                    const int row = 32 * nb + 16 * s2 + 4 * g + ((lane & 15) >> 2), half = (lane & 1) * 8;
+#pragma unroll
+                    for (int d = 0; d < ND; ++d) {
+                        const int c = 4 * d + 2 * (lane >> 4 & 1) + ((lane & 3) >> 1);
+                        const s16x4 a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vt + S::value_slot(row, c) * 16 + half));
+                        const s16x4 a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vt + S::value_slot(row + 8, c) * 16 + half));
+                        const bf16x8 va = __builtin_bit_cast(bf16x8, __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7));
+                        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va, pf, o[d], 0, 0, 0);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int v = 0; v < 16; ++v) {
+                    const int row = 32 * nb + 8 * (v >> 2) + 4 * g + (v & 3);
+#pragma unroll
+                    for (int d = 0; d < ND; ++d) {
+                        const float va = *(const float*)(vt + S::value_slot(row, 8 * d + (j31 >> 2)) * 16 + (j31 & 3) * 4);
+                        o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(va, sc[nb][v], o[d], 0, 0, 0);
+                    }
+                }
+            }
+        }
+#undef EACH_SCORE
+#undef KEY_OFFSET
+    };
+
+    if (FEW) {
+        for (int t = t_a + wave; t < t_z; t += 4) {
+            if (t == t_a + wave) fetch(tile_start(t));
+            put(tile_start(t), 0);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            if (t + 4 < t_z) fetch(tile_start(t + 4));
+            compute(tile_start(t), 0, p.doc_k != nullptr);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        }
+    } else {
+        int buf = 0;
+        for (int base = t_a; base < t_z; base += 64) {
+            const int m = t_z - base < 64 ? t_z - base : 64;
+            unsigned long long live = m == 64 ? ~0ull : (1ull << m) - 1, masked = 0;
+            if (p.doc_k) {
+                // (every wave looks at all of them: the answer is the same, and nobody waits for another)
+                unsigned long long l = 0;
+#pragma unroll 8
+                for (int i = 0; i < m; ++i) {
+                    const int j = tile_start(base + i) + (KT == 64 ? lane : j31), d = j < n ? p.doc_k[k0 + j] : -1;
+                    if (__any(d >= doc_lo && d <= doc_hi)) l |= 1ull << i;
+                    if (!(doc_one && __all(d == doc_lo))) masked |= 1ull << i;
+                }
+                live = l;
+            }
+            if (!live) continue;
+            int t = __builtin_ctzll(live);
+            fetch(tile_start(base + t));
+            for (;;) {
+                const int j0 = tile_start(base + t);
+                const bool doc_mask = masked >> t & 1;
+                put(j0, buf);
+                live &= live - 1;
+                barrier_lds();
+                if (live) {
+                    t = __builtin_ctzll(live);
+                    fetch(tile_start(base + t));
+                }
+                if (!idle) compute(j0, buf, doc_mask);
+                buf ^= 1;
+                if (!live) break;
+            }
         }
     }
-    const float inv = l > 0.f ? 1.f / l : 0.f;
-    E* out = (E*)p.out + t * p.out_token + h * p.out_head;
-    if (lane < p.width) out[lane] = (E)(o0 * inv);
-    if (lane + 64 < p.width) out[lane + 64] = (E)(o1 * inv);
-    if (p.lse && lane == 0) p.lse[(size_t)t * p.heads + h] = l > 0.f ? m + logf(l) : -INFINITY;
+
+    // ---- results ----
+    {
+        float l = lrun, h = lrun;
+        swap_halves(l, h);
+        lrun = l + h;
+    }
+    float m2 = mrun == -INFINITY ? -INFINITY : mrun * mult;     // base-2 units
+    if (FEW) {
+        // The waves' sums, 32 rows x DP each in the wave's own tile (chunk c of row r in slot c ^ (r % 16)), maxima and sums behind
+        float* ml = (float*)(lds + S::JOIN);
+        barrier_lds();                                      // (documents are read no more)
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int v4 = 0; v4 < 4; ++v4) {
+                const int c = 8 * d + 2 * v4 + g;
+                *(f32x4*)(mine + (j31 * (DP / 4) + (c ^ (j31 & 15))) * 16) = f32x4{o[d][4 * v4], o[d][4 * v4 + 1], o[d][4 * v4 + 2], o[d][4 * v4 + 3]};
+            }
+        if (g == 0) {
+            ml[(wave * 32 + j31) * 2] = m2;
+            ml[(wave * 32 + j31) * 2 + 1] = lrun;
+        }
+        barrier_lds();
+        constexpr int TPR = 8, CPT = DP / 4 / TPR;          // threads of a row, chunks of four of each
+        const int row = tid / TPR, cc = tid % TPR;
+        if (row >= rows) return;
+        float top = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) top = __builtin_fmaxf(top, ml[(w * 32 + row) * 2]);
+        float f[4], sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float m = ml[(w * 32 + row) * 2];
+            f[w] = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+            sum += f[w] * ml[(w * 32 + row) * 2 + 1];
+        }
+        const int qu = row / p.share, he = hk * p.share + row - qu * p.share;
+        const size_t at = (size_t)(q0 + qu) * p.heads + he;
+        const float inv = p.splits > 1 ? 1.f : sum > 0.f ? 1.f / sum : 0.f;
+#pragma unroll
+        for (int i = 0; i < CPT; ++i) {
+            const int c = cc + TPR * i;
+            if (c * 4 >= p.width) continue;
+            f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const f32x4 y = *(const f32x4*)(lds + w * 2 * S::TILE + (row * (DP / 4) + (c ^ (row & 15))) * 16);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] += f[w] * y[e];
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] *= inv;
+            if (p.splits > 1) {
+                *(f32x4*)(p.part + ((size_t)split * p.total_q * p.heads + at) * DP + c * 4) = x;
+            } else {
+                E* out = (E*)(p.out + (size_t)(q0 + qu) * p.ot + (size_t)he * p.oh) + c * 4;
+                if constexpr (S::B16) *(bf16x4*)out = bf16x4{(bf16)x[0], (bf16)x[1], (bf16)x[2], (bf16)x[3]};
+                else *(f32x4*)out = x;
+            }
+        }
+        if (cc == 0) {
+            if (p.splits > 1) {
+                float* to = p.part_ml + ((size_t)split * p.total_q * p.heads + at) * 2;
+                to[0] = top;
+                to[1] = sum;
+            } else if (p.lse) {
+                p.lse[at] = sum > 0.f ? (top + __builtin_log2f(sum)) * kLn2 : -INFINITY;
+            }
+        }
+        return;
+    }
+    const size_t at = (size_t)(q0 + query) * p.heads + head;
+    if (p.splits > 1) {
+        if (r >= rows) return;
+        const size_t row = (size_t)split * p.total_q * p.heads + at;
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int v4 = 0; v4 < 4; ++v4)
+                *(f32x4*)(p.part + row * DP + 32 * d + 8 * v4 + 4 * g) = f32x4{o[d][4 * v4], o[d][4 * v4 + 1], o[d][4 * v4 + 2], o[d][4 * v4 + 3]};
+        if (g == 0) {
+            p.part_ml[row * 2] = m2;
+            p.part_ml[row * 2 + 1] = lrun;
+        }
+        return;
+    }
+    if (g == 0 && r < rows && p.lse) p.lse[at] = lrun > 0.f ? (m2 + __builtin_log2f(lrun)) * kLn2 : -INFINITY;
+    barrier_lds();                                          // (the tiles are read no more)
+    if (idle) return;
+    // The wave's 32 rows leave through its quarter of the tiles as whole rows.
+    const float inv = lrun > 0.f ? 1.f / lrun : 0.f;
+    char* stage = lds + wave * kWaveRows * RC * 16;
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int v4 = 0; v4 < 4; ++v4) {
+            const int byte = (32 * d + 8 * v4 + 4 * g) * (int)sizeof(E), c = byte >> 4;
+            char* to = stage + (j31 * RC + (c ^ (RC == 8 ? j31 & 7 : j31 & 15))) * 16 + (byte & 15);
+            if constexpr (S::B16)
+                *(bf16x4*)to = bf16x4{(bf16)(o[d][4 * v4] * inv), (bf16)(o[d][4 * v4 + 1] * inv), (bf16)(o[d][4 * v4 + 2] * inv), (bf16)(o[d][4 * v4 + 3] * inv)};
+            else
+                *(f32x4*)to = f32x4{o[d][4 * v4] * inv, o[d][4 * v4 + 1] * inv, o[d][4 * v4 + 2] * inv, o[d][4 * v4 + 3] * inv};
+        }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    constexpr int RPI = 64 / RC;                            // rows an instruction stores
+    const int oc = lane % RC;
+    if (oc * 16 < p.width * (int)sizeof(E))
+#pragma unroll
+        for (int x = 0; x < kWaveRows; x += RPI) {
+            const int row = x + lane / RC, rr = rw + row;
+            if (rr >= rows) break;
+            const int qu = rr / p.share, he = hk * p.share + rr - qu * p.share;
+            *(u32x4*)(p.out + (size_t)(q0 + qu) * p.ot + (size_t)he * p.oh + oc * 16) = *(const u32x4*)(stage + (row * RC + (oc ^ (RC == 8 ? row & 7 : row & 15))) * 16);
+        }
+}
+
+// A wave joins the parts of one query and head.
+template <class E, int DP>
+__global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs p)
+{
+    const int lane = threadIdx.x & 63, b = blockIdx.z, head = blockIdx.y, r = blockIdx.x * 4 + (threadIdx.x >> 6);
+    int q0, nq;
+    sequence_range(p.cu_q[b], p.cu_q[b + 1], p.total_q, p.max_q, q0, nq);
+    if (r >= nq) return;
+    const size_t step = (size_t)p.total_q * p.heads, at = (size_t)(q0 + r) * p.heads + head;
+    float top = -INFINITY;
+    for (int s = lane; s < p.splits; s += 64) top = __builtin_fmaxf(top, p.part_ml[(s * step + at) * 2]);
+    top = wave_max(top);
+    float sum = 0.f, x0 = 0.f, x1 = 0.f;
+#pragma unroll 4
+    for (int s = 0; s < p.splits; ++s) {
+        const float m = p.part_ml[(s * step + at) * 2], f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+        sum += f * p.part_ml[(s * step + at) * 2 + 1];
+        const float* x = p.part + (s * step + at) * DP;
+        x0 += f * x[lane];
+        if (DP > 64) x1 += f * x[lane + 64];
+    }
+    const float inv = sum > 0.f ? 1.f / sum : 0.f;
+    E* out = (E*)(p.out + (size_t)(q0 + r) * p.ot + (size_t)head * p.oh);
+    if (lane < p.width) out[lane] = (E)(x0 * inv);
+    if (DP > 64 && lane + 64 < p.width) out[lane + 64] = (E)(x1 * inv);
+    if (p.lse && lane == 0) p.lse[at] = sum > 0.f ? (top + __builtin_log2f(sum)) * kLn2 : -INFINITY;
+}
+
+struct Plan {
+    bool few;
+    int dp, items, splits;
+    size_t part, ml;                    // bytes
+};
+
+// Parts of a call: as many as give every compute unit two workgroups, of at least 256 keys for each wave (few rows) or 512 for all of them.
+Plan make_plan(const sp_attention_args& a)
+{
+    Plan P{};
+    const int share = a.heads / a.kv_heads;
+    P.few = (int64_t)a.max_q * share <= kWaveRows;
+    P.dp = a.width <= 64 ? 64 : 128;
+    P.items = P.few ? a.batch : (int)((int64_t)a.total_q * share / kManyRows) + a.batch;
+    const int64_t blocks = P.few ? (int64_t)a.batch * a.kv_heads
+                                 : ((int64_t)a.max_q * share + kManyRows - 1) / kManyRows * a.batch * a.kv_heads;
+    const int64_t want = (512 + blocks - 1) / blocks, most = a.max_k / (P.few ? 1024 : 512);
+    P.splits = (int)(want < most ? want : most);
+    P.splits = P.splits < 1 ? 1 : P.splits > 64 ? 64 : P.splits;
+    if (P.splits > 1) {
+        const size_t rows = (size_t)P.splits * a.total_q * a.heads;
+        P.part = rows * P.dp * 4;
+        P.ml = rows * 8;
+    }
+    return P;
+}
+
+template <class E, int DP, bool FEW>
+hipError_t launch_shape(const AttendArgs& a, const Plan& P, hipStream_t s)
+{
+    const size_t smem = Shape<E, DP, FEW>::LDS + (!FEW && a.table ? (size_t)a.share * (2 * (a.reach + kTablePad) + 1) * 4 : 0);
+    auto kern = attend_kernel<E, DP, FEW>;
+    static std::atomic<size_t> raised{0};                   // per instantiation; the attribute is sticky for the process
+    if (smem > 48 * 1024 && raised.load(std::memory_order_acquire) < smem) {
+        const size_t most = Shape<E, DP, FEW>::LDS + (FEW ? 0 : kTableBytes);
+        const hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)most);
+        if (e != hipSuccess) return e;
+        raised.store(most, std::memory_order_release);
+    }
+    const dim3 grid = FEW ? dim3((unsigned)a.batch, (unsigned)a.kv_heads, (unsigned)P.splits)
+                          : dim3((unsigned)(((int64_t)P.items * a.kv_heads * P.splits + 7) / 8 * 8));
+    hipLaunchKernelGGL(kern, grid, dim3(256), smem, s, a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || P.splits == 1) return e;
+    hipLaunchKernelGGL((attend_join_kernel<E, DP>), dim3((unsigned)((a.max_q + 3) / 4), (unsigned)a.heads, (unsigned)a.batch), dim3(256), 0, s, a);
+    return hipGetLastError();
+}
+
+template <class E>
+hipError_t launch_type(const AttendArgs& a, const Plan& P, hipStream_t s)
+{
+    if (P.dp == 64) return P.few ? launch_shape<E, 64, true>(a, P, s) : launch_shape<E, 64, false>(a, P, s);
+    return P.few ? launch_shape<E, 128, true>(a, P, s) : launch_shape<E, 128, false>(a, P, s);
 }
 
 }  // namespace
 
-size_t attend_workspace_bytes(const sp_attention_args&) { return 0; }
-
-hipError_t launch_attend(const sp_attention_args& a, void*, hipStream_t s)
+size_t attend_workspace_bytes(const sp_attention_args& a)
 {
-    const dim3 grid((unsigned)((a.max_q + 3) / 4), (unsigned)a.heads, (unsigned)a.batch);
-    if (a.dtype == SP_DTYPE_FP32) hipLaunchKernelGGL(attend_simple_kernel<float>, grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL(attend_simple_kernel<bf16>, grid, dim3(256), 0, s, a);
-    return hipGetLastError();
+    const Plan P = make_plan(a);
+    return P.part + P.ml;
+}
+
+hipError_t launch_attend(const sp_attention_args& a, void* workspace, hipStream_t s)
+{
+    const Plan P = make_plan(a);
+    const size_t sz = a.dtype == SP_DTYPE_FP32 ? 4 : 2;
+    AttendArgs d{};
+    d.q = (const char*)a.q; d.k = (const char*)a.k; d.v = (const char*)a.v; d.out = (char*)a.out; d.lse = a.lse;
+    d.qt = a.q_token * sz; d.qh = a.q_head * sz; d.kt = a.k_token * sz; d.kh = a.k_head * sz;
+    d.vt = a.v_token * sz; d.vh = a.v_head * sz; d.ot = a.out_token * sz; d.oh = a.out_head * sz;
+    d.cu_q = a.cu_q; d.cu_k = a.cu_k; d.prefix = a.prefix; d.q_first = a.q_first; d.doc_q = a.doc_q; d.doc_k = a.doc_k;
+    d.slopes = a.slopes; d.bias = a.bias;
+    d.part = (float*)workspace; d.part_ml = (float*)((char*)workspace + P.part);
+    d.scale = a.scale; d.cap = a.cap;
+    d.batch = a.batch; d.heads = a.heads; d.kv_heads = a.kv_heads; d.share = a.heads / a.kv_heads; d.width = a.width;
+    d.total_q = a.total_q; d.total_k = a.total_k; d.max_q = a.max_q; d.max_k = a.max_k; d.left = a.left; d.right = a.right; d.reach = a.reach;
+    d.items = P.items; d.splits = P.splits;
+    d.table = a.bias && (int64_t)d.share * (2 * ((int64_t)a.reach + kTablePad) + 1) * 4 <= kTableBytes;
+    return a.dtype == SP_DTYPE_FP32 ? launch_type<float>(d, P, s) : launch_type<bf16>(d, P, s);
 }
 
 }  // namespace sp
@@ -89,13 +652,15 @@ int check_attention(const sp_attention_args* a)
     if (a->dtype != SP_DTYPE_FP32 && a->dtype != SP_DTYPE_BF16) return SP_EINVAL;
     if (a->batch < 0 || a->heads < 1 || a->kv_heads < 1 || a->heads % a->kv_heads || a->heads > 65535) return SP_ESHAPE;
     if (a->width < 8 || a->width > 128 || a->width % 8) return SP_ESHAPE;
-    if (a->batch > 65535 || a->total_q < 0 || a->total_k < 0 || a->max_q < 0 || a->max_k < 0) return SP_ESHAPE;
+    constexpr int32_t most = 1 << 29;                      // (positions and distances stay inside 32 bits)
+    if (a->batch > 65535 || a->total_q > most || a->total_k > most || a->total_q < 0 || a->total_k < 0 || a->max_q < 0 || a->max_k < 0) return SP_ESHAPE;
+    if ((int64_t)a->total_q * a->heads > (1 << 30) || (int64_t)a->batch * a->heads > (1 << 24)) return SP_ESHAPE;
     if (!std::isfinite(a->scale) || !std::isfinite(a->cap) || a->reach < 0 || a->reach > (1 << 20)) return SP_EINVAL;
     if (!a->doc_q != !a->doc_k) return SP_EINVAL;
     const int sz = a->dtype == SP_DTYPE_FP32 ? 4 : 2;
     const int64_t strides[] = {a->q_token, a->q_head, a->k_token, a->k_head, a->v_token, a->v_head, a->out_token, a->out_head};
     for (int64_t s : strides) {
-        if (s < 0) return SP_ESHAPE;
+        if (s < 0 || s > most) return SP_ESHAPE;
         if (s * sz & 15) return SP_EINVAL;
     }
     if (!rows_apart(a->total_q, a->out_token, a->heads, a->out_head, a->width)) return SP_ESHAPE;
