@@ -21,22 +21,59 @@ namespace sp {
 namespace {
 
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.69314718055994531f;
-constexpr int kWaveRows = 32, kManyRows = 128;
+constexpr int kWaveRows = 32;
+enum { kMany, kSmall, kFew };          // shapes of a workgroup: 4 x 32 rows, 2 x 32 rows, 32 rows with the keys shared out to four waves
 constexpr int kTablePad = 96;           // entries on each side of the table in LDS: a wave's 32 rows and a tile's 64 keys are less than that apart
+constexpr int kRun = 16;                // neighbouring workgroups that stay on one XCD
 constexpr int kTableBytes = 14336;      // largest table in LDS
+
+// cap tanh(scale s / cap) in base-2 units; cap2 = cap log2(e), pre = scale / cap (fp32) or 2 log2(e) scale / cap (bf16)
+template <class E>
+__device__ __forceinline__ float capped(float s, float pre, float cap2)
+{
+    if (sizeof(E) == 4) return cap2 * tanhf(s * pre);
+    // tanh(y) = 1 - 2 / (e^(2 y) + 1): 2^-23 off in absolute value, far inside what bf16 operands leave of a score
+    return __builtin_fmaf(-2.f * cap2, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(s * pre) + 1.f), cap2);
+}
+
+// The same for |scale s / cap| < kNearCap, where five full-rate instructions do for two at a quarter of it and three more:
+// tanh(y) = y (1 + y^2 (a + y^2 (b + y^2 c))), coefficients in terms of s
+constexpr float kNearCap = 0.4f;
+struct NearCap {
+    float k0, k1, k2, k3;
+};
+__device__ __forceinline__ float capped_near(float s, const NearCap& k)
+{
+    const float t = s * s;
+    return s * __builtin_fmaf(t, __builtin_fmaf(t, __builtin_fmaf(t, k.k3, k.k2), k.k1), k.k0);
+}
 
 struct AttendArgs {
     const char *q, *k, *v;
     char* out;
     float* lse;
-    size_t qt, qh, kt, kh, vt, vh, ot, oh;                  // strides in bytes
+    size_t qt, qh, kh, vh, ot, oh;                          // strides in bytes
+    int kt, vt;
     const int32_t *cu_q, *cu_k, *prefix, *q_first, *doc_q, *doc_k;
     const float *slopes, *bias;
     float *part, *part_ml;                                  // [splits][total_q * heads][DP] sums, and (maximum, sum) pairs
-    float scale, cap;
-    int batch, heads, kv_heads, share, width, total_q, total_k, max_q, max_k, left, right, reach;
+    // Scores in base-2 units: raw ones (nothing but a positive scale) are multiplied where the exponential is taken.  cap2: the cap; pre: see
+    // capped(); near_cap: |s| below which capped_near() does.
+    float mult, pre, cap2, near_cap;
+    NearCap cap_near;
+    int raw, batch, heads, kv_heads, share, width, total_q, total_k, max_q, max_k, left, right, reach;
     int items, splits, table;                               // table: whether the bias is in LDS
 };
+
+// Sixteen bytes per lane from base + soff (uniform) + voff, zeros from `bytes` on.
+__device__ __forceinline__ u32x4 load16_bounded(const char* base, int bytes, int voff, int soff)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    return __builtin_amdgcn_raw_buffer_load_b128(__builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), 0, bytes, 0x00020000), voff, soff, 0);
+#else
+    return u32x4{};
+#endif
+}
 
 __device__ __forceinline__ void sequence_range(int t0, int t1, int total, int most, int& at, int& n)
 {
@@ -49,43 +86,45 @@ __device__ __forceinline__ void sequence_range(int t0, int t1, int total, int mo
 // A bias in units of the base-2 logarithm; finite ones stay finite.
 __device__ __forceinline__ float in_log2(float b) { return __builtin_isinf(b) ? b : __builtin_amdgcn_fmed3f(b * kLog2e, -3.0e38f, 3.0e38f); }
 
-template <class E>
-__device__ __forceinline__ float capped(float s, float cap, float inv_cap)
-{
-    if (sizeof(E) == 4) return cap * tanhf(s * inv_cap);
-    // tanh(y) = 1 - 2 / (e^(2 y) + 1): 2^-23 off in absolute value, far inside what bf16 operands leave of a score
-    return __builtin_fmaf(-2.f * cap, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(s * (2.f * kLog2e * inv_cap)) + 1.f), cap);
-}
-
-template <class E, int DP, bool FEW>
+template <class E, int DP, int KIND>
 struct Shape {
-    static constexpr bool B16 = sizeof(E) == 2;
-    static constexpr int KT = FEW || !B16 ? 32 : 64;        // keys of a tile
-    static constexpr int NT = FEW ? 64 : 256;               // threads that fetch it
+    static constexpr bool B16 = sizeof(E) == 2, FEW = KIND == kFew;
+    static constexpr int WAVES = KIND == kSmall ? 2 : 4, ROWS = FEW ? kWaveRows : WAVES * kWaveRows;
+    static constexpr int KT = KIND == kMany && B16 ? 64 : 32;       // keys of a tile
+    static constexpr int NT = FEW ? 64 : WAVES * 64;        // threads that fetch it
     static constexpr int RC = DP * (int)sizeof(E) / 16;     // 16-byte chunks of a row
     static constexpr int LPT = KT * RC / NT, RS = NT / RC;  // chunks a thread fetches, rows between them
     static constexpr int TILE = KT * RC * 16;               // bytes
     static constexpr int BUFS = FEW ? 4 : 2;                // FEW: one of each wave
-    static constexpr int DOCS = BUFS * 2 * TILE, TABLE = DOCS + BUFS * KT * 4;      // offsets in LDS
+    static constexpr int DOCS = BUFS * 2 * TILE, FOUND = DOCS + BUFS * KT * 4,
+                         TABLE = FOUND + 128;                // offsets in LDS (FOUND: see the loop over tiles)
     static constexpr int JOIN = DOCS;                       // (FEW: maxima and sums of the waves, over the documents)
-    static constexpr size_t LDS = TABLE + (FEW ? 1024 - BUFS * KT * 4 : 0);
-    static_assert(BUFS * 2 * TILE >= 4 * kWaveRows * DP * (FEW ? 4 : (int)sizeof(E)), "the outputs reuse the tiles");
-    // Chunk c of row r is in slot c ^ swizzle(r): the sixteen rows that a quarter of a read takes, or the four rows by four chunks of a
-    // transposing one, lie in different banks.
-    static __device__ __forceinline__ int key_slot(int r, int c) { return r * RC + (c ^ (RC == 8 ? (r >> 1) & 7 : r & 15)); }
-    static __device__ __forceinline__ int value_slot(int r, int c)
-    {
-        return r * RC + (c ^ (!B16 ? (r >> 2 & 1) << 3 : RC == 8 ? (r >> 1 & 1) << 2 : (r & 3) << 2));
-    }
+    static constexpr size_t LDS = FEW ? DOCS + 1024 : TABLE;
+    static_assert(BUFS * 2 * TILE >= WAVES * kWaveRows * DP * (FEW ? 4 : (int)sizeof(E)), "the outputs reuse the tiles");
+    // Chunk c of row r is in slot c ^ turn(r): the sixteen rows that a quarter of a read takes, or the four rows by four chunks of a
+    // transposing one, lie in different banks.  Both turns are made of bits of r, so that of r + r' with no bit in common is the
+    // exclusive or of theirs.
+    static __host__ __device__ constexpr int key_turn(int r) { return RC == 8 ? (r >> 1) & 7 : r & 15; }
+    static __host__ __device__ constexpr int value_turn(int r) { return !B16 ? (r >> 2 & 1) << 3 : RC == 8 ? (r >> 1 & 1) << 2 : (r & 3) << 2; }
+    static __device__ __forceinline__ int key_slot(int r, int c) { return r * RC + (c ^ key_turn(r)); }
+    static __device__ __forceinline__ int value_slot(int r, int c) { return r * RC + (c ^ value_turn(r)); }
 };
+
+// Waves on a SIMD that the registers are shared out for.
+constexpr int waves_per_simd(bool b16, int dp, int kind)
+{
+    return kind == kFew ? (!b16 && dp == 128 ? 1 : 2) : kind == kSmall ? (b16 && dp == 64 ? 4 : 2) : b16 && dp == 64 ? 3 : 2;
+}
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
-template <class E, int DP, bool FEW>
-__global__ __launch_bounds__(256, FEW ? (sizeof(E) == 4 && DP == 128 ? 1 : 2) : (DP == 64 && sizeof(E) == 2 ? 3 : 2)) void attend_kernel(AttendArgs p)
+template <class E, int DP, int KIND>
+__global__ __launch_bounds__((Shape<E, DP, KIND>::WAVES * 64), waves_per_simd(sizeof(E) == 2, DP, KIND)) void attend_kernel(AttendArgs p)
 {
-    using S = Shape<E, DP, FEW>;
+    using S = Shape<E, DP, KIND>;
+    constexpr bool FEW = S::FEW;
+    constexpr int ROWS = S::ROWS, SHIFT = ROWS == 128 ? 7 : 6;
     constexpr int KT = S::KT, NB = KT / 32, RC = S::RC, LPT = S::LPT, RS = S::RS, ND = DP / 32;
     extern __shared__ char lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), j31 = lane & 31, g = lane >> 5;
@@ -100,24 +139,30 @@ __global__ __launch_bounds__(256, FEW ? (sizeof(E) == 4 && DP == 128 ? 1 : 2) : 
         c0 = p.cu_q[b];
         c1 = p.cu_q[b + 1];
     } else {
-        // Neighbouring items of one key head read the same keys: contiguous runs per XCD (workgroup id mod 8).
-        const int total = p.items * p.kv_heads * p.splits, chunk = (total + 7) >> 3;
-        const int lin = (int)(blockIdx.x & 7) * chunk + (int)(blockIdx.x >> 3);
-        if ((int)(blockIdx.x >> 3) >= chunk || lin >= total) return;
+        // Neighbouring items of one key head read the same keys: runs of kRun stay on one XCD (workgroup id mod 8) and go round the XCDs,
+        // another way each time, so that these have the same work whatever the lengths.  The last items come first: behind a causal
+        // mask they are the longest, and what runs last should be short.
+        const int total = p.items * p.kv_heads * p.splits, y = (int)(gridDim.x >> 3) - 1 - (int)(blockIdx.x >> 3), round = y / kRun;
+        const int lin = (round * 8 + (((int)blockIdx.x + round) & 7)) * kRun + y % kRun;
+        if (lin >= total) return;
         split = lin % p.splits;
         const int item = lin / p.splits % p.items;
         hk = lin / p.splits / p.items;
-        // Item i belongs to the last sequence with cu * share / 128 + b <= i: every sequence gets as many as it has blocks of rows, at least
-        b = last_sequence(p.cu_q, p.batch, lane, [&](int i, int c) { return ((int64_t)c * p.share >> 7) + i <= item; }, c0, c1);
-        const int64_t start = (int64_t)item - (((int64_t)c0 * p.share >> 7) + b);
+        // Item i belongs to the last sequence with cu * share / ROWS + b <= i: every sequence gets as many as it has blocks of rows, at least
+        b = last_sequence(p.cu_q, p.batch, lane, [&](int i, int c) { return ((int64_t)c * p.share >> SHIFT) + i <= item; }, c0, c1);
+        const int64_t start = (int64_t)item - (((int64_t)c0 * p.share >> SHIFT) + b);
         if (start < 0 || start > (1 << 23)) return;
-        r0 = (int)start * kManyRows;
+        r0 = (int)start * ROWS;
     }
     sequence_range(c0, c1, p.total_q, p.max_q, q0, nq);
     const int rows = nq * p.share;
     if (r0 >= rows) return;                                 // (the whole workgroup)
     int k0, n;
-    sequence_range(p.cu_k[b], p.cu_k[b + 1], p.total_k, p.max_k, k0, n);
+    if (p.cu_k != p.cu_q) {                                 // (self-attention: the same offsets)
+        c0 = p.cu_k[b];
+        c1 = p.cu_k[b + 1];
+    }
+    sequence_range(c0, c1, p.total_k, p.max_k, k0, n);
     int first = p.q_first ? p.q_first[b] : n - nq;
     first = first < -(1 << 30) ? -(1 << 30) : first > 1 << 30 ? 1 << 30 : first;
     int prefix = p.prefix ? p.prefix[b] : 0;
@@ -136,7 +181,7 @@ __global__ __launch_bounds__(256, FEW ? (sizeof(E) == 4 && DP == 128 ? 1 : 2) : 
     const int any_lo = first_seen(pos_a), any_hi = last_seen(pos_z), all_lo = first_seen(pos_z), all_hi = last_seen(pos_a);
 
     // ---- which key tiles: those of the prefix, then those of the window of all the workgroup's rows ----
-    const int re = r0 + (FEW ? kWaveRows : kManyRows) - 1 < rows ? r0 + (FEW ? kWaveRows : kManyRows) - 1 : rows - 1;
+    const int re = r0 + ROWS - 1 < rows ? r0 + ROWS - 1 : rows - 1;
     const int w_lo = first_seen(first + r0 / p.share), w_hi = last_seen(first + re / p.share);
     const int tiles1 = (prefix + KT - 1) / KT, from2 = w_lo / KT > tiles1 ? w_lo / KT : tiles1, to2 = (w_hi + KT) / KT;     // (w_hi >= -1)
     const int tiles = tiles1 + (w_hi >= w_lo && to2 > from2 ? to2 - from2 : 0);
@@ -154,19 +199,13 @@ __global__ __launch_bounds__(256, FEW ? (sizeof(E) == 4 && DP == 128 ? 1 : 2) : 
     }
     const int doc = p.doc_q ? p.doc_q[q0 + query] : 0;
     const float slope = p.slopes ? p.slopes[head] * kLog2e : 0.f;
-    const float* brow = p.bias ? p.bias + (size_t)head * (2 * p.reach + 1) : nullptr;
-    const float bias_left = brow ? in_log2(brow[0]) : 0.f, bias_right = brow ? in_log2(brow[2 * p.reach]) : 0.f;
+    float bias_left = 0.f, bias_right = 0.f;
+    if (p.bias) {
+        bias_left = in_log2(p.bias[(size_t)head * (2 * p.reach + 1)]);
+        bias_right = in_log2(p.bias[(size_t)head * (2 * p.reach + 1) + 2 * p.reach]);
+    }
     float* table = (float*)(lds + S::TABLE);
     const int pitch = 2 * (p.reach + kTablePad) + 1;
-    if (!FEW && p.table) {
-        for (int h = 0; h < p.share; ++h)
-            for (int e = tid; e < pitch; e += 256) {
-                int d = e - kTablePad;
-                d = d < 0 ? 0 : d > 2 * p.reach ? 2 * p.reach : d;
-                table[h * pitch + e] = in_log2(p.bias[(size_t)(hk * p.share + h) * (2 * p.reach + 1) + d]);
-            }
-        barrier_lds();
-    }
     const float* tab = table + (head - hk * p.share) * pitch + p.reach + kTablePad;
 
     // ---- documents of the workgroup's rows ----
@@ -193,37 +232,59 @@ __global__ __launch_bounds__(256, FEW ? (sizeof(E) == 4 && DP == 128 ? 1 : 2) : 
 
     // ---- fetching: thread -> chunk fc of rows fr + i RS ----
     const int ft = FEW ? lane : tid, fc = ft % RC, fr = ft / RC;
+    // Buffer loads from a tile's first row, bounded by the sequence's last row: what lies behind it, and chunks behind the width, come as
+    // zeros.  One register of address per lane for each of the two.
     const bool inside = fc * 16 < p.width * (int)sizeof(E);
-    const char* kbase = p.k + (size_t)k0 * p.kt + (size_t)hk * p.kh + fc * 16;
-    const char* vbase = p.v + (size_t)k0 * p.vt + (size_t)hk * p.vh + fc * 16;
+    const int k_at = inside ? fr * p.kt + fc * 16 : INT32_MAX, v_at = inside ? fr * p.vt + fc * 16 : INT32_MAX;
+    const char* kbase = p.k + (size_t)k0 * p.kt + (size_t)hk * p.kh;
+    const char* vbase = p.v + (size_t)k0 * p.vt + (size_t)hk * p.vh;
     u32x4 kr[LPT], vr[LPT];
     int dr[LPT], dk = 0;                                    // documents of the fetched rows; of the tile's key `ft`
-    auto fetch = [&](int j0) {
+    auto fetch = [&](int j0, bool docs) {
+        const int last = n - j0 < KT ? n - j0 - 1 : KT - 1;
+        const int kn = last * p.kt + p.width * (int)sizeof(E), vn = last * p.vt + p.width * (int)sizeof(E);
 #pragma unroll
         for (int i = 0; i < LPT; ++i) {
-            int j = j0 + fr + i * RS;
-            j = j < n ? j : n - 1;
-            if (inside) {
-                kr[i] = *(const u32x4*)(kbase + (size_t)(unsigned)j * (unsigned)p.kt);
-                vr[i] = *(const u32x4*)(vbase + (size_t)(unsigned)j * (unsigned)p.vt);
+            kr[i] = load16_bounded(kbase + (size_t)j0 * p.kt, kn, k_at, i * RS * p.kt);
+            vr[i] = load16_bounded(vbase + (size_t)j0 * p.vt, vn, v_at, i * RS * p.vt);
+            if (docs) {
+                const int j = j0 + fr + i * RS;
+                dr[i] = p.doc_k[k0 + (j < n ? j : n - 1)];
             }
-            if (p.doc_k) dr[i] = p.doc_k[k0 + j];
         }
-        if (p.doc_k && ft < KT) dk = p.doc_k[k0 + (j0 + ft < n ? j0 + ft : n - 1)];
+        if (docs && ft < KT) dk = p.doc_k[k0 + (j0 + ft < n ? j0 + ft : n - 1)];
     };
+    const int key_to = S::key_slot(fr, fc) * 16, value_to = S::TILE + S::value_slot(fr, fc) * 16;
     char* const mine = lds + (FEW ? wave * 2 * S::TILE : 0);
-    auto put = [&](int j0, int buf) {
+    auto put = [&](int j0, int buf, bool docs) {
         char* to = mine + (FEW ? 0 : buf * 2 * S::TILE);
+        if (docs) {                                         // values that no row sees become zeros: a weight of zero does not hide a NaN
+#pragma unroll
+            for (int i = 0; i < LPT; ++i)
+                if (dr[i] < 0) vr[i] = u32x4{0, 0, 0, 0};
+        }
+        int kto = key_to, vto = value_to;
+        asm volatile("" : "+v"(kto), "+v"(vto));
 #pragma unroll
         for (int i = 0; i < LPT; ++i) {
-            const int row = fr + i * RS;
-            // (values that no row sees become zeros: a weight of zero does not hide a NaN)
-            const bool seen = inside && j0 + row < n && !(p.doc_k && dr[i] < 0);
-            *(u32x4*)(to + S::key_slot(row, fc) * 16) = inside ? kr[i] : u32x4{0, 0, 0, 0};
-            *(u32x4*)(to + S::TILE + S::value_slot(row, fc) * 16) = seen ? vr[i] : u32x4{0, 0, 0, 0};
+            constexpr int step = RS * RC * 16;
+            *(u32x4*)(to + (kto ^ S::key_turn(i * RS) * 16) + i * step) = kr[i];
+            *(u32x4*)(to + (vto ^ S::value_turn(i * RS) * 16) + i * step) = vr[i];
         }
-        if (p.doc_k && ft < KT) ((int*)(lds + S::DOCS))[(FEW ? wave : buf) * KT + ft] = dk;
+        if (docs && ft < KT) ((int*)(lds + S::DOCS))[(FEW ? wave : buf) * KT + ft] = dk;
     };
+
+    // The first tile is requested before anything else is waited for.  (With documents it is not known yet.)
+    const bool ahead = !FEW && !p.doc_k && t_a < t_z;
+    if (ahead) fetch(tile_start(t_a), false);
+    if (!FEW && p.table) {
+        for (int h = 0; h < p.share; ++h)
+            for (int e = tid; e < pitch; e += S::NT) {
+                int d = e - kTablePad;
+                d = d < 0 ? 0 : d > 2 * p.reach ? 2 * p.reach : d;
+                table[h * pitch + e] = in_log2(p.bias[(size_t)(hk * p.share + h) * (2 * p.reach + 1) + d]);
+            }
+    }
 
     // ---- one tile ----
     f32x16 o[ND];
@@ -232,22 +293,30 @@ __global__ __launch_bounds__(256, FEW ? (sizeof(E) == 4 && DP == 128 ? 1 : 2) : 
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[d][e] = 0.f;
     float mrun = -INFINITY, lrun = 0.f;                     // (of this half's keys)
-    const bool raw = !(p.cap > 0.f) && !p.slopes && !p.bias && p.scale > 0.f;
-    const float mult = raw ? p.scale * kLog2e : 1.f, pre = p.cap > 0.f ? p.scale : p.scale * kLog2e, inv_cap = p.cap > 0.f ? 1.f / p.cap : 0.f;
+    const bool raw = p.raw;
+    const float mult = p.mult;
+    // Where a lane reads key row j31, chunk g, and values: rows 4 g .. (bf16: a quarter wave's four rows by sixteen dimensions, eight bytes a
+    // lane; fp32: dimension j31).  Rows further on are constants away: the swizzles go by bits of the row below those.
+    const int key_at = S::key_slot(j31, g) * 16;
+    const int value_at = S::TILE + (S::B16 ? S::value_slot(4 * g + ((lane & 15) >> 2), 2 * (lane >> 4 & 1) + ((lane & 3) >> 1)) * 16 + (lane & 1) * 8
+                                           : S::value_slot(4 * g, j31 >> 2) * 16 + (j31 & 3) * 4);
     auto compute = [&](int j0, int buf, bool doc_mask) {
         const bool in_prefix = j0 < prefix;
         if (!in_prefix && (j0 > any_hi || j0 + KT <= any_lo)) return;       // (the wave sees none of it)
-        const char* kt = mine + (FEW ? 0 : buf * 2 * S::TILE);
-        const char* vt = kt + S::TILE;
+        // Addresses of the fragments are exclusive ors of two lane-dependent ones with constants (opaque here: kept in registers, all of
+        // them together would spill).
+        int kat = key_at, vat = value_at;
+        asm volatile("" : "+v"(kat), "+v"(vat));
+        const char* tile = mine + (FEW ? 0 : buf * 2 * S::TILE);
         f32x16 sc[NB];
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) sc[nb][e] = 0.f;
-            const int row = nb * 32 + j31;
 #pragma unroll
             for (int s = 0; s < QF; ++s) {
-                const u32x4 a = *(const u32x4*)(kt + S::key_slot(row, 2 * s + g) * 16);
+                const u32x4 a = *(const u32x4*)(tile + (kat ^ (s * 32)) + nb * 32 * RC * 16);
                 if constexpr (S::B16) {
                     sc[nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, qf[s]), sc[nb], 0, 0, 0);
                 } else {
@@ -257,16 +326,27 @@ __global__ __launch_bounds__(256, FEW ? (sizeof(E) == 4 && DP == 128 ? 1 : 2) : 
                 }
             }
         }
+        __builtin_amdgcn_s_setprio(0);
         // Register v of block nb is key j0 + 32 nb + 8 (v / 4) + 4 g + v % 4.
 #define EACH_SCORE for (int nb = 0; nb < NB; ++nb) _Pragma("unroll") for (int v = 0; v < 16; ++v)
 #define KEY_OFFSET (32 * nb + 8 * (v >> 2) + (v & 3))
         const int jg = j0 + 4 * g;
         if (!raw) {
+            if (p.cap2 > 0.f) {
+                float far = 0.f;
+                if (S::B16)
 #pragma unroll
-            EACH_SCORE sc[nb][v] *= pre;
-            if (p.cap > 0.f) {
+                    EACH_SCORE far = __builtin_fmaxf(far, __builtin_fabsf(sc[nb][v]));
+                if (S::B16 && __all(far < p.near_cap)) {
 #pragma unroll
-                EACH_SCORE sc[nb][v] = capped<E>(sc[nb][v], p.cap, inv_cap) * kLog2e;
+                    EACH_SCORE sc[nb][v] = capped_near(sc[nb][v], p.cap_near);
+                } else {
+#pragma unroll
+                    EACH_SCORE sc[nb][v] = capped<E>(sc[nb][v], p.pre, p.cap2);
+                }
+            } else {
+#pragma unroll
+                EACH_SCORE sc[nb][v] *= p.pre;
             }
             if (p.slopes) {
                 const float d0 = (float)(jg - pos);
@@ -285,11 +365,14 @@ __global__ __launch_bounds__(256, FEW ? (sizeof(E) == 4 && DP == 128 ? 1 : 2) : 
 #pragma unroll
                     EACH_SCORE sc[nb][v] += at[KEY_OFFSET];
                 } else {
+                    // (32-bit offsets, few at a time: registers)
+                    const unsigned at = (unsigned)head * (unsigned)(2 * p.reach + 1) + (unsigned)p.reach;
 #pragma unroll
                     EACH_SCORE {
                         int d = jg + KEY_OFFSET - pos;
                         d = d < -p.reach ? -p.reach : d > p.reach ? p.reach : d;
-                        sc[nb][v] += in_log2(brow[d + p.reach]);
+                        sc[nb][v] += in_log2(p.bias[at + (unsigned)d]);
+                        if (v % 4 == 3) __builtin_amdgcn_sched_barrier(0);
                     }
                 }
             }
@@ -312,7 +395,9 @@ __global__ __launch_bounds__(256, FEW ? (sizeof(E) == 4 && DP == 128 ? 1 : 2) : 
             swap_halves(l, h);
             mx = __builtin_fmaxf(l, h);
         }
-        if (__any(mx > mrun)) {
+        // The reference of the exponentials moves where a row's maximum has outgrown it by 2^8, not with every new maximum (of 32 rows
+        // one has a new one in most tiles): weights up to 2^8 then, with the same relative rounding.
+        if (__any((mx - mrun) * mult > 8.f || (mrun == -INFINITY && mx > mrun))) {
             mx = __builtin_fmaxf(mx, mrun);
             const float alpha = mrun == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mrun - mx) * mult);
             mrun = mx;
@@ -331,6 +416,7 @@ __global__ __launch_bounds__(256, FEW ? (sizeof(E) == 4 && DP == 128 ? 1 : 2) : 
             sc[nb][v] = e;
         }
         lrun += psum;
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
             if constexpr (S::B16) {
@@ -339,12 +425,11 @@ __global__ __launch_bounds__(256, FEW ? (sizeof(E) == 4 && DP == 128 ? 1 : 2) : 
                     bf16x8 pf;
 #pragma unroll
                     for (int e = 0; e < 8; ++e) pf[e] = (bf16)sc[nb][8 * s2 + e];
-                    const int row = 32 * nb + 16 * s2 + 4 * g + ((lane & 15) >> 2), half = (lane & 1) * 8;
 #pragma unroll
                     for (int d = 0; d < ND; ++d) {
-                        const int c = 4 * d + 2 * (lane >> 4 & 1) + ((lane & 3) >> 1);
-                        const s16x4 a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vt + S::value_slot(row, c) * 16 + half));
-                        const s16x4 a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vt + S::value_slot(row + 8, c) * 16 + half));
+                        const char* at = tile + (vat ^ (d * 64)) + (32 * nb + 16 * s2) * RC * 16;
+                        const s16x4 a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)at);
+                        const s16x4 a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(at + 8 * RC * 16));
                         const bf16x8 va = __builtin_bit_cast(bf16x8, __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7));
                         o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va, pf, o[d], 0, 0, 0);
                     }
@@ -352,27 +437,28 @@ __global__ __launch_bounds__(256, FEW ? (sizeof(E) == 4 && DP == 128 ? 1 : 2) : 
             } else {
 #pragma unroll
                 for (int v = 0; v < 16; ++v) {
-                    const int row = 32 * nb + 8 * (v >> 2) + 4 * g + (v & 3);
 #pragma unroll
                     for (int d = 0; d < ND; ++d) {
-                        const float va = *(const float*)(vt + S::value_slot(row, 8 * d + (j31 >> 2)) * 16 + (j31 & 3) * 4);
+                        const float va = *(const float*)(tile + (vat ^ (d * 128)) + (32 * nb + 8 * (v >> 2) + (v & 3)) * RC * 16);
                         o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(va, sc[nb][v], o[d], 0, 0, 0);
                     }
                 }
             }
         }
+        __builtin_amdgcn_s_setprio(0);
 #undef EACH_SCORE
 #undef KEY_OFFSET
     };
 
     if (FEW) {
+        const bool docs = p.doc_k != nullptr;
         for (int t = t_a + wave; t < t_z; t += 4) {
-            if (t == t_a + wave) fetch(tile_start(t));
-            put(tile_start(t), 0);
+            if (t == t_a + wave) fetch(tile_start(t), docs);
+            put(tile_start(t), 0, docs);
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
-            if (t + 4 < t_z) fetch(tile_start(t + 4));
-            compute(tile_start(t), 0, p.doc_k != nullptr);
+            if (t + 4 < t_z) fetch(tile_start(t + 4), docs);
+            compute(tile_start(t), 0, docs);
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
         }
@@ -382,28 +468,55 @@ __global__ __launch_bounds__(256, FEW ? (sizeof(E) == 4 && DP == 128 ? 1 : 2) : 
             const int m = t_z - base < 64 ? t_z - base : 64;
             unsigned long long live = m == 64 ? ~0ull : (1ull << m) - 1, masked = 0;
             if (p.doc_k) {
-                // (every wave looks at all of them: the answer is the same, and nobody waits for another)
-                unsigned long long l = 0;
-#pragma unroll 8
-                for (int i = 0; i < m; ++i) {
-                    const int j = tile_start(base + i) + (KT == 64 ? lane : j31), d = j < n ? p.doc_k[k0 + j] : -1;
-                    if (__any(d >= doc_lo && d <= doc_hi)) l |= 1ull << i;
-                    if (!(doc_one && __all(d == doc_lo))) masked |= 1ull << i;
+                // Four keys a lane, so that a load covers 256 of them; each wave looks at its share of the 64 tiles.  (Two places in LDS in turn:
+                // a wave is at most one barrier ahead.)
+                constexpr int LPK = KT / 4, TPL = 64 / LPK, OWN = 64 / S::WAVES;        // lanes of a tile, tiles of a load, tiles of a wave
+                unsigned long long l = 0, u = 0;
+#pragma unroll
+                for (int i = 0; i < OWN; i += TPL) {
+                    const int x0 = wave * OWN + i, t = x0 + lane / LPK, j = tile_start(base + (t < m ? t : m - 1)) + lane % LPK * 4;
+                    bool any = false, all = doc_one;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int d = p.doc_k[k0 + (j + e < n ? j + e : n - 1)];
+                        any = any || (d >= doc_lo && d <= doc_hi && j + e < n);
+                        all = all && d == doc_lo && j + e < n;
+                    }
+                    const unsigned long long some = __ballot(any), full = __ballot(all);
+                    constexpr unsigned long long one = (1ull << LPK) - 1;
+#pragma unroll
+                    for (int x = 0; x < TPL; ++x) {
+                        if (some >> x * LPK & one) l |= 1ull << (x0 + x);
+                        if ((full >> x * LPK & one) != one) u |= 1ull << (x0 + x);
+                    }
                 }
-                live = l;
+                unsigned long long* found = (unsigned long long*)(lds + S::FOUND) + (base - t_a >> 6 & 1) * 8;
+                if (lane == 0) {
+                    found[wave] = l;
+                    found[4 + wave] = u;
+                }
+                barrier_lds();
+                l = 0;
+#pragma unroll
+                for (int w = 0; w < S::WAVES; ++w) {
+                    l |= found[w];
+                    masked |= found[4 + w];
+                }
+                live &= ((unsigned long long)(unsigned)__builtin_amdgcn_readfirstlane((int)(l >> 32)) << 32) | (unsigned)__builtin_amdgcn_readfirstlane((int)l);
+                masked = ((unsigned long long)(unsigned)__builtin_amdgcn_readfirstlane((int)(masked >> 32)) << 32) | (unsigned)__builtin_amdgcn_readfirstlane((int)masked);
             }
             if (!live) continue;
             int t = __builtin_ctzll(live);
-            fetch(tile_start(base + t));
+            if (!ahead || base > t_a) fetch(tile_start(base + t), masked >> t & 1);
             for (;;) {
                 const int j0 = tile_start(base + t);
                 const bool doc_mask = masked >> t & 1;
-                put(j0, buf);
+                put(j0, buf, doc_mask);
                 live &= live - 1;
                 barrier_lds();
                 if (live) {
                     t = __builtin_ctzll(live);
-                    fetch(tile_start(base + t));
+                    fetch(tile_start(base + t), masked >> t & 1);
                 }
                 if (!idle) compute(j0, buf, doc_mask);
                 buf ^= 1;
@@ -558,22 +671,23 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs p)
 }
 
 struct Plan {
-    bool few;
-    int dp, items, splits;
+    int kind, dp, items, splits;
     size_t part, ml;                    // bytes
 };
 
-// Parts of a call: as many as give every compute unit two workgroups, of at least 256 keys for each wave (few rows) or 512 for all of them.
+// Shape of the workgroups: few rows where no sequence has more than 32, small where they have up to 96 on average (of 128 rows half
+// the waves would be idle).  Parts of a call: as many as give every compute unit two workgroups, of at least 256 keys for each wave (few
+// rows) or 512 for all of them.
 Plan make_plan(const sp_attention_args& a)
 {
     Plan P{};
     const int share = a.heads / a.kv_heads;
-    P.few = (int64_t)a.max_q * share <= kWaveRows;
+    P.kind = (int64_t)a.max_q * share <= kWaveRows ? kFew : (int64_t)a.total_q * share <= (int64_t)96 * a.batch ? kSmall : kMany;
     P.dp = a.width <= 64 ? 64 : 128;
-    P.items = P.few ? a.batch : (int)((int64_t)a.total_q * share / kManyRows) + a.batch;
-    const int64_t blocks = P.few ? (int64_t)a.batch * a.kv_heads
-                                 : ((int64_t)a.max_q * share + kManyRows - 1) / kManyRows * a.batch * a.kv_heads;
-    const int64_t want = (512 + blocks - 1) / blocks, most = a.max_k / (P.few ? 1024 : 512);
+    const int rows = P.kind == kMany ? 128 : 64;
+    P.items = P.kind == kFew ? a.batch : (int)((int64_t)a.total_q * share / rows) + a.batch;
+    const int64_t blocks = P.kind == kFew ? (int64_t)a.batch * a.kv_heads : ((int64_t)a.max_q * share + rows - 1) / rows * a.batch * a.kv_heads;
+    const int64_t want = (512 + blocks - 1) / blocks, most = a.max_k / (P.kind == kFew ? 1024 : 512);
     P.splits = (int)(want < most ? want : most);
     P.splits = P.splits < 1 ? 1 : P.splits > 64 ? 64 : P.splits;
     if (P.splits > 1) {
@@ -584,32 +698,38 @@ Plan make_plan(const sp_attention_args& a)
     return P;
 }
 
-template <class E, int DP, bool FEW>
+template <class E, int DP, int KIND>
 hipError_t launch_shape(const AttendArgs& a, const Plan& P, hipStream_t s)
 {
-    const size_t smem = Shape<E, DP, FEW>::LDS + (!FEW && a.table ? (size_t)a.share * (2 * (a.reach + kTablePad) + 1) * 4 : 0);
-    auto kern = attend_kernel<E, DP, FEW>;
+    using S = Shape<E, DP, KIND>;
+    const size_t smem = S::LDS + (!S::FEW && a.table ? (size_t)a.share * (2 * (a.reach + kTablePad) + 1) * 4 : 0);
+    auto kern = attend_kernel<E, DP, KIND>;
     static std::atomic<size_t> raised{0};                   // per instantiation; the attribute is sticky for the process
     if (smem > 48 * 1024 && raised.load(std::memory_order_acquire) < smem) {
-        const size_t most = Shape<E, DP, FEW>::LDS + (FEW ? 0 : kTableBytes);
+        const size_t most = S::LDS + (S::FEW ? 0 : kTableBytes);
         const hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, (int)most);
         if (e != hipSuccess) return e;
         raised.store(most, std::memory_order_release);
     }
-    const dim3 grid = FEW ? dim3((unsigned)a.batch, (unsigned)a.kv_heads, (unsigned)P.splits)
-                          : dim3((unsigned)(((int64_t)P.items * a.kv_heads * P.splits + 7) / 8 * 8));
-    hipLaunchKernelGGL(kern, grid, dim3(256), smem, s, a);
+    const dim3 grid = S::FEW ? dim3((unsigned)a.batch, (unsigned)a.kv_heads, (unsigned)P.splits)
+                          : dim3((unsigned)(((int64_t)P.items * a.kv_heads * P.splits + 8 * kRun - 1) / (8 * kRun) * (8 * kRun)));
+    hipLaunchKernelGGL(kern, grid, dim3(S::WAVES * 64), smem, s, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || P.splits == 1) return e;
     hipLaunchKernelGGL((attend_join_kernel<E, DP>), dim3((unsigned)((a.max_q + 3) / 4), (unsigned)a.heads, (unsigned)a.batch), dim3(256), 0, s, a);
     return hipGetLastError();
 }
 
+template <class E, int DP>
+hipError_t launch_kind(const AttendArgs& a, const Plan& P, hipStream_t s)
+{
+    return P.kind == kFew ? launch_shape<E, DP, kFew>(a, P, s) : P.kind == kSmall ? launch_shape<E, DP, kSmall>(a, P, s) : launch_shape<E, DP, kMany>(a, P, s);
+}
+
 template <class E>
 hipError_t launch_type(const AttendArgs& a, const Plan& P, hipStream_t s)
 {
-    if (P.dp == 64) return P.few ? launch_shape<E, 64, true>(a, P, s) : launch_shape<E, 64, false>(a, P, s);
-    return P.few ? launch_shape<E, 128, true>(a, P, s) : launch_shape<E, 128, false>(a, P, s);
+    return P.dp == 64 ? launch_kind<E, 64>(a, P, s) : launch_kind<E, 128>(a, P, s);
 }
 
 }  // namespace
@@ -626,12 +746,19 @@ hipError_t launch_attend(const sp_attention_args& a, void* workspace, hipStream_
     const size_t sz = a.dtype == SP_DTYPE_FP32 ? 4 : 2;
     AttendArgs d{};
     d.q = (const char*)a.q; d.k = (const char*)a.k; d.v = (const char*)a.v; d.out = (char*)a.out; d.lse = a.lse;
-    d.qt = a.q_token * sz; d.qh = a.q_head * sz; d.kt = a.k_token * sz; d.kh = a.k_head * sz;
-    d.vt = a.v_token * sz; d.vh = a.v_head * sz; d.ot = a.out_token * sz; d.oh = a.out_head * sz;
+    d.qt = a.q_token * sz; d.qh = a.q_head * sz; d.kt = (int)(a.k_token * sz); d.kh = a.k_head * sz;
+    d.vt = (int)(a.v_token * sz); d.vh = a.v_head * sz; d.ot = a.out_token * sz; d.oh = a.out_head * sz;
     d.cu_q = a.cu_q; d.cu_k = a.cu_k; d.prefix = a.prefix; d.q_first = a.q_first; d.doc_q = a.doc_q; d.doc_k = a.doc_k;
     d.slopes = a.slopes; d.bias = a.bias;
     d.part = (float*)workspace; d.part_ml = (float*)((char*)workspace + P.part);
-    d.scale = a.scale; d.cap = a.cap;
+    const float ratio = a.cap > 0.f ? a.scale / a.cap : 0.f, k0 = a.scale * kLog2e, r2 = ratio * ratio;
+    d.raw = !(a.cap > 0.f) && !a.slopes && !a.bias && a.scale > 0.f;
+    d.mult = d.raw ? k0 : 1.f;
+    d.cap2 = a.cap > 0.f ? a.cap * kLog2e : 0.f;
+    d.pre = a.cap > 0.f ? ratio * (sz == 2 ? 2.f * kLog2e : 1.f) : k0;
+    d.near_cap = kNearCap / std::fabs(ratio);
+    // (the least-squares fit of tanh(y) on |y| < 0.4, reweighted until its errors were even: 2.8e-8)
+    d.cap_near = NearCap{k0, -0.33331388f * k0 * r2, 0.13268751f * k0 * r2 * r2, -0.04742304f * k0 * r2 * r2 * r2};
     d.batch = a.batch; d.heads = a.heads; d.kv_heads = a.kv_heads; d.share = a.heads / a.kv_heads; d.width = a.width;
     d.total_q = a.total_q; d.total_k = a.total_k; d.max_q = a.max_q; d.max_k = a.max_k; d.left = a.left; d.right = a.right; d.reach = a.reach;
     d.items = P.items; d.splits = P.splits;
@@ -656,6 +783,7 @@ int check_attention(const sp_attention_args* a)
     if (a->batch > 65535 || a->total_q > most || a->total_k > most || a->total_q < 0 || a->total_k < 0 || a->max_q < 0 || a->max_k < 0) return SP_ESHAPE;
     if ((int64_t)a->total_q * a->heads > (1 << 30) || (int64_t)a->batch * a->heads > (1 << 24)) return SP_ESHAPE;
     if (!std::isfinite(a->scale) || !std::isfinite(a->cap) || a->reach < 0 || a->reach > (1 << 20)) return SP_EINVAL;
+    if (a->bias && (int64_t)a->heads * (2 * (int64_t)a->reach + 1) > (1 << 30)) return SP_ESHAPE;
     if (!a->doc_q != !a->doc_k) return SP_EINVAL;
     const int sz = a->dtype == SP_DTYPE_FP32 ? 4 : 2;
     const int64_t strides[] = {a->q_token, a->q_head, a->k_token, a->k_head, a->v_token, a->v_head, a->out_token, a->out_head};
@@ -663,6 +791,7 @@ int check_attention(const sp_attention_args* a)
         if (s < 0 || s > most) return SP_ESHAPE;
         if (s * sz & 15) return SP_EINVAL;
     }
+    if (a->k_token > (1 << 23) || a->v_token > (1 << 23)) return SP_ESHAPE;         // (offsets inside a tile of 64 rows are 32-bit)
     if (!rows_apart(a->total_q, a->out_token, a->heads, a->out_head, a->width)) return SP_ESHAPE;
     const void* rows[] = {a->q, a->k, a->v, a->out};
     for (const void* p : rows)
