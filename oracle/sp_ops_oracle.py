@@ -7,6 +7,7 @@ from __future__ import annotations
 import math
 
 import numpy as np
+import torch
 
 HALF_STEP = {"bf16": 2.0 ** -8, "fp32": 2.0 ** -24}     # of a rounding, relative to the value
 F32 = 2.0 ** -24
@@ -36,7 +37,7 @@ def linear_int8(x, w_codes, w_scales, bias=None, residual=None, gelu=False, dtyp
         y = y + np.asarray(bias, np.float64)
     off = off + 2 * F32 * np.abs(y)
     if gelu:
-        y = y * 0.5 * np.vectorize(math.erfc)(-y / math.sqrt(2.0))
+        y = y * 0.5 * torch.erfc(torch.from_numpy(-y / math.sqrt(2.0))).numpy()
         off = 1.13 * off + 4e-7
     if residual is not None:
         y = y + np.asarray(residual, np.float64)

@@ -34,6 +34,8 @@ struct Int8Args {
     size_t a_ss, as_ss, w_ss, ws_ss, b_ss, res_ss, out_ss;      // bytes
     int tokens, N, Kd, groups;
 };
+bool linear_int8_fused(int tokens, int Kd);
+hipError_t launch_linear_int8_fused(const Int8Args& a, const void* x, int64_t x_row, int dtype, int epilogue, hipStream_t s);
 hipError_t launch_gemm_int8(const Int8Args& a, int dtype, int epilogue, hipStream_t s);
 
 size_t attend_workspace_bytes(const sp_attention_args& a);

@@ -10,7 +10,9 @@ gradient: inputs that require one are refused while gradients are recorded.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import math
+import struct
 
 import numpy as np
 import torch
@@ -33,6 +35,11 @@ class sp_attention_args(C.Structure):
         (n, C.c_void_p) for n in ("prefix", "q_first", "doc_q", "doc_k", "slopes", "bias")] + [("reach", C.c_int32)]
 
 
+# The same for struct.pack, which fills it several times faster than the fields one by one.
+_ATTENTION = struct.Struct("@5P8q2P9i2f2i6Pi0P")
+assert _ATTENTION.size == C.sizeof(sp_attention_args)
+
+
 def _load() -> C.CDLL:
     lib = _sp.raw_lib()
     vp, i32, i64, sz, f32, f64 = C.c_void_p, C.c_int32, C.c_int64, C.c_size_t, C.c_float, C.c_double
@@ -44,8 +51,8 @@ def _load() -> C.CDLL:
     lib.sp_rotary_frequencies.argtypes = [i32, f64, i32, f64, f64, vp, C.POINTER(f32)]
     lib.sp_rotary.restype = C.c_int
     lib.sp_rotary.argtypes = [vp, i64, i64, vp, i64, i64, i32, i32, i32, i32, i32, i32, vp, f32, vp, vp, i32, vp]
-    lib.sp_attention_workspace_bytes.restype = sz; lib.sp_attention_workspace_bytes.argtypes = [C.POINTER(sp_attention_args)]
-    lib.sp_attention.restype = C.c_int; lib.sp_attention.argtypes = [C.POINTER(sp_attention_args), vp, sz, vp]
+    lib.sp_attention_workspace_bytes.restype = sz; lib.sp_attention_workspace_bytes.argtypes = [vp]
+    lib.sp_attention.restype = C.c_int; lib.sp_attention.argtypes = [vp, vp, sz, vp]
     return lib
 
 
@@ -58,54 +65,76 @@ def _need(ok: bool, what: str) -> None:
         raise ValueError(what)
 
 
-def _home(first: torch.Tensor, *others) -> torch.device:
-    """The device that all tensors are on."""
-    dev = first.device
-    _need(dev.type == "cuda", "the tensors have to be on a GPU: there is no CPU path in this library")
-    recording = torch.is_grad_enabled()
-    for t in (first, *others):
+_raw_stream = torch._C._cuda_getCurrentRawStream
+_recording = torch.is_grad_enabled
+_bytes_of = functools.lru_cache(maxsize=4096)(_lib.sp_linear_int8_workspace_bytes)
+
+
+def _home(first: torch.Tensor, *others) -> int:
+    """The index of the device that all tensors are on."""
+    dev = first.get_device()
+    _need(dev >= 0, "the tensors have to be on a GPU: there is no CPU path in this library")
+    recording = _recording()
+    if recording and first.requires_grad:
+        raise ValueError("this operator has no gradient: call it under torch.no_grad() or on detached tensors")
+    for t in others:
         if t is not None:
-            _need(t.device == dev, f"tensors on {t.device} and {dev}")
-            _need(not (recording and t.requires_grad), "this operator has no gradient: call it under torch.no_grad() or on detached tensors")
+            if t.get_device() != dev:
+                raise ValueError(f"tensors on {t.device} and {first.device}")
+            if recording and t.requires_grad:
+                raise ValueError("this operator has no gradient: call it under torch.no_grad() or on detached tensors")
     return dev
 
 
 class _On:
-    """The device made current for the call where it is not (a context manager; nothing is done in the usual case)."""
+    """The device made current for the call where it is not."""
     __slots__ = ("index", "before")
 
-    def __init__(self, dev: torch.device):
-        self.index = dev.index
+    def __init__(self, index: int):
+        self.index = index
 
     def __enter__(self):
         self.before = torch.cuda.current_device()
-        if self.before != self.index:
-            torch.cuda.set_device(self.index)
-        return torch.cuda.current_stream(self.index).cuda_stream
+        torch.cuda.set_device(self.index)
 
     def __exit__(self, *_):
-        if self.before != self.index:
-            torch.cuda.set_device(self.before)
+        torch.cuda.set_device(self.before)
+
+
+def _call(dev: int, fn, *args) -> None:
+    """fn(*args, stream) on the current stream of the device, with the device current."""
+    if torch._C._cuda_getDevice() == dev:
+        rc = fn(*args, _raw_stream(dev))
+    else:
+        with _On(dev):
+            rc = fn(*args, _raw_stream(dev))
+    if rc:
+        raise SpError(rc)
 
 
 def _dtype(t: torch.Tensor) -> int:
     d = _DTYPES.get(t.dtype)
-    _need(d is not None, f"float32 or bfloat16 is wanted, not {t.dtype}")
+    if d is None:
+        raise ValueError(f"float32 or bfloat16 is wanted, not {t.dtype}")
     return d
 
 
 def _vector(t, name: str, dtype, n: int):
     if t is None:
         return None
-    _need(t.dtype == dtype and t.dim() == 1 and t.numel() == n and t.is_contiguous(), f"{name}: a contiguous {dtype} vector of {n} is wanted")
+    if t.dtype is not dtype or t.dim() != 1 or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name}: a contiguous {dtype} vector of {n} is wanted")
     return t.data_ptr()
 
 
 def _rows(t: torch.Tensor, name: str, shape, dtype) -> int:
     """The row stride of a matrix whose rows are contiguous."""
-    _need(t.dtype == dtype and tuple(t.shape) == tuple(shape), f"{name}: {dtype} of shape {tuple(shape)} is wanted, not {t.dtype} {tuple(t.shape)}")
-    _need(t.shape[1] <= 1 or t.stride(1) == 1, f"{name}: the elements of a row have to be contiguous")
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    if t.dtype is not dtype or t.shape != shape:
+        raise ValueError(f"{name}: {dtype} of shape {tuple(shape)} is wanted, not {t.dtype} {tuple(t.shape)}")
+    row, one = t.stride()
+    if one != 1 and shape[1] > 1:
+        raise ValueError(f"{name}: the elements of a row have to be contiguous")
+    return row if shape[0] > 1 else shape[1]
 
 
 # ---- 8-bit integers ---------------------------------------------------------------------------------------------
@@ -118,12 +147,11 @@ def quantize_int8(x: torch.Tensor):
     rows, width = x.shape
     x_row = _rows(x, "x", x.shape, x.dtype)
     pad = (width + 15) // 16 * 16
-    with _On(dev) as stream:
-        codes = torch.empty(rows, pad, dtype=torch.int8, device=dev)
-        if pad > width:
-            codes[:, width:].zero_()
-        scales = torch.empty(rows, dtype=torch.float32, device=dev)
-        _check(_lib.sp_quantize_int8(x.data_ptr(), x_row, dtype, rows, width, codes.data_ptr(), pad, scales.data_ptr(), stream))
+    codes = torch.empty(rows, pad, dtype=torch.int8, device=x.device)
+    if pad > width:
+        codes[:, width:].zero_()
+    scales = torch.empty(rows, dtype=torch.float32, device=x.device)
+    _call(dev, _lib.sp_quantize_int8, x.data_ptr(), x_row, dtype, rows, width, codes.data_ptr(), pad, scales.data_ptr())
     return codes[:, :width], scales
 
 
@@ -135,28 +163,33 @@ def linear_int8(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, bias
     dtype, dev = _dtype(x), _home(x, codes, scales, bias, residual, out)
     _need(x.dim() == 2 and codes.dim() == 2, "x and codes: matrices are wanted")
     T, K = x.shape
-    N = codes.shape[0]
-    _need(codes.dtype == torch.int8 and codes.shape[1] == K, f"codes: int8 [width_out, {K}] is wanted")
+    N, Kw = codes.shape
+    _need(codes.dtype is torch.int8 and Kw == K, "codes: int8 [width_out, width_in] is wanted")
     _need(K >= 1 and N >= 1, "codes: at least one row and one column are wanted")
     pad = (K + 15) // 16 * 16
-    w_row = codes.stride(0) if N > 1 else pad
-    _need(K == 1 or codes.stride(1) == 1, "codes: the elements of a row have to be contiguous")
-    _need(w_row % 16 == 0 and codes.data_ptr() % 16 == 0, "codes: rows have to start at multiples of 16 bytes (see quantize_int8)")
-    _need((N - 1) * w_row + pad + codes.storage_offset() <= codes.untyped_storage().nbytes(),
+    w_row, w_one = codes.stride()
+    if N == 1:
+        w_row = pad
+    w = codes.data_ptr()
+    _need(K == 1 or w_one == 1, "codes: the elements of a row have to be contiguous")
+    _need(w_row % 16 == 0 and w % 16 == 0, "codes: rows have to start at multiples of 16 bytes (see quantize_int8)")
+    _need(pad == K or (N - 1) * w_row + pad + codes.storage_offset() <= codes.untyped_storage().nbytes(),
           "codes: the last row's storage has to reach to the next multiple of 16 (see quantize_int8)")
     _need(not (gelu and residual is not None), "gelu or residual, not both")
-    x_row = _rows(x, "x", (T, K), x.dtype)
-    r_row = _rows(residual, "residual", (T, N), x.dtype) if residual is not None else 0
+    shape = (T, N)
+    x_row = _rows(x, "x", x.shape, x.dtype)
+    r, r_row, epilogue = None, 0, LINEAR_GELU if gelu else LINEAR_PLAIN
+    if residual is not None:
+        r, r_row, epilogue = residual.data_ptr(), _rows(residual, "residual", shape, x.dtype), LINEAR_RESIDUAL
     sc, bi = _vector(scales, "scales", torch.float32, N), _vector(bias, "bias", torch.float32, N)
-    with _On(dev) as stream:
-        if out is None:
-            out = torch.empty(T, N, dtype=x.dtype, device=dev)
-        o_row = _rows(out, "out", (T, N), x.dtype)
-        need = _lib.sp_linear_int8_workspace_bytes(T, K)
-        ws = torch.empty(need, dtype=torch.uint8, device=dev)
-        _check(_lib.sp_linear_int8(x.data_ptr(), x_row, dtype, T, K, codes.data_ptr(), w_row, sc, N, bi,
-                                   LINEAR_GELU if gelu else LINEAR_RESIDUAL if residual is not None else LINEAR_PLAIN,
-                                   residual.data_ptr() if residual is not None else None, r_row, out.data_ptr(), o_row, ws.data_ptr(), need, stream))
+    if out is None:
+        out, o_row = x.new_empty(shape), N
+    else:
+        o_row = _rows(out, "out", shape, x.dtype)
+    need = _bytes_of(T, K)
+    ws = torch.empty(need, dtype=torch.uint8, device=x.device)
+    _call(dev, _lib.sp_linear_int8, x.data_ptr(), x_row, dtype, T, K, w, w_row, sc, N, bi, epilogue, r, r_row, out.data_ptr(), o_row,
+          ws.data_ptr(), need)
     return out
 
 
@@ -179,23 +212,27 @@ def rotary(x: torch.Tensor, frequencies: torch.Tensor, *, positions: torch.Tenso
     in place.  Tokens of no sequence stay as they were in `out` and are unspecified in an output that is made here."""
     dtype, dev = _dtype(x), _home(x, frequencies, positions, cu_seqlens, out)
     _need(x.dim() == 3 and x.shape[1] >= 1 and x.shape[2] >= 2, "x: [tokens, heads, width] is wanted")
-    _need(layout in ROTARY_LAYOUTS, f"layout: one of {', '.join(ROTARY_LAYOUTS)}")
+    way = ROTARY_LAYOUTS.get(layout)
+    _need(way is not None, "layout: half or interleaved")
     _need((positions is None) != (cu_seqlens is None), "positions or cu_seqlens: one of the two")
     T, A, D = x.shape
-    _need(x.stride(2) == 1, "x: the elements of a head have to be contiguous")
-    fr = _vector(frequencies, "frequencies", torch.float64, frequencies.numel())
-    pos = _vector(positions, "positions", torch.int32, T)
-    batch, cu = 0, None
-    if cu_seqlens is not None:
+    x_token, x_head, one = x.stride()
+    _need(one == 1, "x: the elements of a head have to be contiguous")
+    half = frequencies.numel()
+    fr = _vector(frequencies, "frequencies", torch.float64, half)
+    batch, pos, cu = 0, None, None
+    if positions is not None:
+        pos = _vector(positions, "positions", torch.int32, T)
+    else:
         batch = cu_seqlens.numel() - 1
         _need(batch >= 0, "cu_seqlens: [batch + 1] is wanted")
         cu = _vector(cu_seqlens, "cu_seqlens", torch.int32, batch + 1)
-    with _On(dev) as stream:
-        if out is None:
-            out = torch.empty(T, A, D, dtype=x.dtype, device=dev)
-        _need(out.dtype == x.dtype and out.shape == x.shape and out.stride(2) == 1, "out: like x")
-        _check(_lib.sp_rotary(x.data_ptr(), x.stride(0), x.stride(1), out.data_ptr(), out.stride(0), out.stride(1), dtype, T, A, D,
-                              2 * frequencies.numel(), ROTARY_LAYOUTS[layout], fr, float(factor), pos, cu, batch, stream))
+    if out is None:
+        out, o_token, o_head = x.new_empty((T, A, D)), A * D, D
+    else:
+        _need(out.dtype is x.dtype and out.shape == x.shape and out.stride(2) == 1, "out: like x")
+        o_token, o_head, _ = out.stride()
+    _call(dev, _lib.sp_rotary, x.data_ptr(), x_token, x_head, out.data_ptr(), o_token, o_head, dtype, T, A, D, 2 * half, way, fr, factor, pos, cu, batch)
     return out
 
 
@@ -218,9 +255,10 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.Ten
     dtype = _dtype(q)
     _need(q.dim() == 3 and k.dim() == 3 and v.dim() == 3, "q, k, v: [tokens, heads, width] is wanted")
     Tq, A, D = q.shape
-    Tk, G = k.shape[0], k.shape[1]
-    _need(k.dtype == q.dtype and v.dtype == q.dtype and k.shape[2] == D and v.shape == k.shape, "k and v: of q's type and width, and of one shape")
-    _need(q.stride(2) == 1 and k.stride(2) == 1 and v.stride(2) == 1, "q, k, v: the elements of a head have to be contiguous")
+    Tk, G, Dk = k.shape
+    _need(k.dtype is q.dtype and v.dtype is q.dtype and Dk == D and v.shape == k.shape, "k and v: of q's type and width, and of one shape")
+    (q_token, q_head, q1), (k_token, k_head, k1), (v_token, v_head, v1) = q.stride(), k.stride(), v.stride()
+    _need(q1 == k1 == v1 == 1, "q, k, v: the elements of a head have to be contiguous")
     batch = cu_q.numel() - 1
     _need(batch >= 0, "cu_q: [batch + 1] is wanted")
     if cu_k is None:
@@ -229,34 +267,32 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.Ten
         doc_k = doc_q if doc_k is None else doc_k
     _need(max_k is not None, "max_k is wanted with cu_k")
     _need((doc_q is None) == (doc_k is None), "doc_q and doc_k: both or none")
-    left, right = (-1, -1) if window is None else (int(window[0]), int(window[1]))
+    left, right = (-1, -1) if window is None else window
     if causal:
         _need(right <= 0, "causal: no keys to the right")
         right = 0
-    reach = 0
+    reach, bi = 0, None
     if bias is not None:
-        _need(bias.dtype == torch.float32 and bias.dim() == 2 and bias.shape[0] == A and bias.shape[1] % 2 == 1 and bias.is_contiguous(),
-              f"bias: contiguous float32 [{A}, 2 reach + 1] is wanted")
-        reach = bias.shape[1] // 2
-    a = sp_attention_args(
-        q=q.data_ptr(), k=k.data_ptr(), v=v.data_ptr(), q_token=q.stride(0), q_head=q.stride(1), k_token=k.stride(0), k_head=k.stride(1),
-        v_token=v.stride(0), v_head=v.stride(1), cu_q=_vector(cu_q, "cu_q", torch.int32, batch + 1), cu_k=_vector(cu_k, "cu_k", torch.int32, batch + 1),
-        dtype=dtype, batch=batch, heads=A, kv_heads=G, width=D, total_q=Tq, total_k=Tk, max_q=int(max_q), max_k=int(max_k),
-        scale=1.0 / math.sqrt(D) if scale is None else float(scale), cap=float(cap), left=max(left, -1), right=max(right, -1),
-        prefix=_vector(prefix, "prefix", torch.int32, batch), q_first=_vector(q_first, "q_first", torch.int32, batch),
-        doc_q=_vector(doc_q, "doc_q", torch.int32, Tq), doc_k=_vector(doc_k, "doc_k", torch.int32, Tk),
-        slopes=_vector(slopes, "slopes", torch.float32, A), bias=bias.data_ptr() if bias is not None else None, reach=reach)
-    with _On(dev) as stream:
-        lse = None
-        if out is None:
-            out = torch.empty(Tq, A, D, dtype=q.dtype, device=dev)
-        else:
-            _need(out.dtype == q.dtype and out.shape == q.shape and out.stride(2) == 1, "out: like q")
-        a.out, a.out_token, a.out_head = out.data_ptr(), out.stride(0), out.stride(1)
-        if with_lse:
-            lse = torch.empty(Tq, A, dtype=torch.float32, device=dev)
-            a.lse = lse.data_ptr()
-        need = _lib.sp_attention_workspace_bytes(C.byref(a))
-        ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
-        _check(_lib.sp_attention(C.byref(a), ws.data_ptr() if need else None, need, stream))
+        _need(bias.dtype is torch.float32 and bias.dim() == 2 and bias.shape[0] == A and bias.shape[1] % 2 == 1 and bias.is_contiguous(),
+              "bias: contiguous float32 [heads, 2 reach + 1] is wanted")
+        reach, bi = bias.shape[1] // 2, bias.data_ptr()
+    if out is None:
+        out, o_token, o_head = q.new_empty((Tq, A, D)), A * D, D
+    else:
+        _need(out.dtype is q.dtype and out.shape == q.shape and out.stride(2) == 1, "out: like q")
+        o_token, o_head, _ = out.stride()
+    lse = torch.empty((Tq, A), dtype=torch.float32, device=q.device) if with_lse else None
+    try:
+        args = _ATTENTION.pack(
+            q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), lse.data_ptr() if with_lse else 0, q_token, q_head, k_token, k_head, v_token, v_head,
+            o_token, o_head, _vector(cu_q, "cu_q", torch.int32, batch + 1), _vector(cu_k, "cu_k", torch.int32, batch + 1), dtype, batch, A, G, D, Tq, Tk,
+            max_q, max_k, 1.0 / math.sqrt(D) if scale is None else scale, cap, left if left > -1 else -1, right if right > -1 else -1,
+            _vector(prefix, "prefix", torch.int32, batch) or 0, _vector(q_first, "q_first", torch.int32, batch) or 0,
+            _vector(doc_q, "doc_q", torch.int32, Tq) or 0, _vector(doc_k, "doc_k", torch.int32, Tk) or 0,
+            _vector(slopes, "slopes", torch.float32, A) or 0, bi or 0, reach)
+    except (struct.error, OverflowError, TypeError) as e:
+        raise ValueError(f"a size or number that does not fit its field: {e}") from None
+    need = _lib.sp_attention_workspace_bytes(args)
+    ws = torch.empty(need, dtype=torch.uint8, device=q.device).data_ptr() if need else None
+    _call(dev, _lib.sp_attention, args, ws, need)
     return (out, lse) if with_lse else out

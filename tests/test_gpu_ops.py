@@ -78,7 +78,7 @@ def test_quantize_strided_and_in_place_width():
 
 
 LINEAR_SIZES = [(1, 1, 1), (1, 16, 3), (1, 768, 2304), (2, 100, 33), (5, 128, 64), (16, 1000, 129), (17, 257, 777), (31, 64, 1000), (33, 384, 256),
-                (63, 129, 65), (64, 1024, 512), (65, 127, 127), (128, 256, 128), (129, 640, 130), (200, 2048, 96), (257, 96, 300), (700, 130, 513), (1999, 72, 77)]
+                (63, 129, 65), (64, 1024, 512), (65, 127, 127), (128, 256, 128), (129, 640, 130), (200, 2048, 96), (257, 96, 300), (700, 130, 513), (1999, 72, 77), (2100, 130, 1030), (4090, 500, 4010)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])

@@ -71,7 +71,7 @@ def attend(**k):
                               scale=1.0, left=-1, right=-1)
     for n, v in k.items():
         setattr(a, n, v)
-    return LIB.sp_attention(C.byref(a), None, 0, None)
+    return LIB.sp_attention(C.addressof(a), None, 0, None)
 
 
 @pytest.mark.parametrize("change,code", [
