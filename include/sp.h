@@ -39,7 +39,7 @@ enum {
     SP_ETOOBIG = -8   /* sp_forward_static: the call needs more workspace than the library's static array holds */
 };
 
-enum { SP_DTYPE_FP32 = 0, SP_DTYPE_BF16 = 1, SP_DTYPE_FP8 = 2 };
+enum { SP_DTYPE_FP32 = 0, SP_DTYPE_BF16 = 1, SP_DTYPE_FP8 = 2, SP_DTYPE_INT8 = 3 };
 
 /* Shape of the student group.  All students share one architecture (Section 3.1:
  * homogeneous students so that none is a straggler). */
@@ -64,7 +64,12 @@ typedef struct {
                          FFN activations exist only in fp8), fp32 accumulation, same epilogues.  Attention
                          itself, the first-token last layer, the head, all smaller calls, and students whose
                          hidden or FFN width is not a multiple of 256 stay bf16 (the arena keeps both copies
-                         of the four matrices). */
+                         of the four matrices);
+                         SP_DTYPE_INT8: quantised students in 8-bit integers, in the same calls and places: the four
+                         projections' weights quantised at load with a scale per output feature, their inputs row by
+                         row with a scale per token (the quantisation and the product are sp_quantize_int8 and
+                         sp_linear_int8 of sp_ops.h); every activation also exists in bf16, and any widths that the bf16
+                         path takes will do. */
     float ln_eps;     /* LayerNorm epsilon (BERT: 1e-12) */
     int32_t last_layer_all_tokens;
                       /* Only the first token of each sequence feeds the head (the pooled representation of
@@ -175,6 +180,29 @@ int sp_forward_static(const sp_model* model, const int32_t* token_ids, const int
                       int32_t batch, int32_t total_tokens, int32_t max_seqlen, int32_t k_active,
                       float* logits_out, void* hip_stream);
 
+/* Another form of attention for all layers of a loaded group, in place of softmax(q k^T / 8) v over all tokens of a sequence: rotary
+ * positions, capped scores, a window, and biases by distance, as defined with sp_rotary and sp_attention in sp_ops.h
+ * (scale 1/8, queries and keys of a sequence being the same tokens).  Null: back to the plain form.
+ * The arrays are device memory of the caller, read by every forward until the form is replaced or the group freed.  Not to be called
+ * while a call on the model is being issued by another thread; calls issued before keep the form they were issued with.
+ * With a form every layer is computed for all tokens, in separate launches, whatever the size of the call (the learned position table of the
+ * blob is still added: zeros there leave positions to the form); first-token rows, split sequences and fused layers are the plain
+ * form's alone.  Quantised students (SP_DTYPE_FP8) compute the output projection in bf16.  The value slice of `qkv`
+ * (sp_ws_layout) is written, `vt` is not.
+ * Errors: SP_EINVAL (null or misaligned arrays, a cap that is not finite), SP_ESHAPE (rotary_dim odd or beyond 64, reach out of 0..2^20). */
+typedef struct {
+    int32_t rotary_dim;                 /* elements of a head that are rotated, 0: none */
+    int32_t rotary_layout;              /* SP_ROTARY_HALF or SP_ROTARY_INTERLEAVED (sp_ops.h) */
+    const double* rotary_frequencies;   /* [rotary_dim / 2] */
+    float rotary_factor;                /* on the rotated values (1, or what sp_rotary_frequencies says) */
+    float cap;                          /* <= 0: none */
+    int32_t left, right;                /* furthest keys that are seen, negative: no bound */
+    const float* slopes;                /* [K][heads] or null */
+    const float* bias;                  /* [K][heads][2 reach + 1] or null */
+    int32_t reach;
+} sp_attention_form;
+int sp_set_attention_form(sp_model* model, const sp_attention_form* form);
+
 /* Releases the host handle only; the arena stays the caller's. */
 void sp_free(sp_model* model);
 
@@ -225,7 +253,7 @@ int sp_check_inputs(const sp_model* model, const int32_t* token_ids, const int32
  *     all; x1 and g are not written;
  *   - bf16 students of hidden 256 and FFN 512 (768, 1024), calls of more than 256 tokens (and of
  *     1280, 1664 tokens x students and more): x1 and g are not written;
- *   - quantised students, calls of >= 2048 token rows: att is not written (attq is);
+ *   - students quantised in fp8, calls of >= 2048 token rows: att is not written (attq is);
  *   - bf16 calls of fewer than 8192 tokens: qkv, vt and att may hold the fp32 slices of a split
  *     reduction;
  *   - a last layer on the first-token rows: in calls of fewer than 1024 tokens its rows lie in qkv,

@@ -62,13 +62,10 @@ def rotary(x, frequencies, positions, layout="half", factor=1.0, dtype="fp32"):
 
 
 def visible(m, n, first, left, right, prefix, doc_q, doc_k):
-    see = np.zeros((m, n), bool)
-    for r in range(m):
-        for j in range(n):
-            d = j - (first + r)
-            see[r, j] = ((left < 0 or d >= -left) and (right < 0 or d <= right)) or j < prefix
-            if doc_q is not None:
-                see[r, j] &= doc_q[r] == doc_k[j] and doc_k[j] >= 0
+    j, d = np.arange(n)[None], np.arange(n)[None] - (first + np.arange(m))[:, None]
+    see = ((d >= -left) | (left < 0)) & ((d <= right) | (right < 0)) | (j < prefix)
+    if doc_q is not None:
+        see = see & (np.asarray(doc_q)[:, None] == np.asarray(doc_k)[None]) & (np.asarray(doc_k)[None] >= 0)
     return see
 
 

@@ -9,7 +9,7 @@
 #include <vector>
 
 #include "sp_dispatch.h"
-#include "sp_internal.h"
+#include "sp_ops_internal.h"
 
 namespace sp {
 
@@ -21,7 +21,8 @@ static bool config_ok(const sp_config* c)
     if (c->K < 1 || c->layers < 1 || c->hidden < 1 || c->heads < 1 || c->ffn < 1 || c->vocab < 1 || c->max_pos < 1 ||
         c->classes < 1)
         return false;
-    if (c->dtype != SP_DTYPE_FP32 && c->dtype != SP_DTYPE_BF16 && c->dtype != SP_DTYPE_FP8) return false;
+    if (c->dtype != SP_DTYPE_FP32 && c->dtype != SP_DTYPE_BF16 && c->dtype != SP_DTYPE_FP8 && c->dtype != SP_DTYPE_INT8)
+        return false;
     if (!(c->ln_eps >= 0.f)) return false;
     return true;
 }
@@ -39,7 +40,7 @@ ArenaLayout make_arena_layout(const sp_config& c)
 {
     const size_t H = c.hidden, F = c.ffn, C = c.classes;
     const size_t wb = bf16_path(c) ? 2 : 4;  // bytes per matrix / table element
-    const size_t q8 = c.dtype == SP_DTYPE_FP8 ? 1 : 0;     // fp8 copies of three matrices
+    const size_t q8 = c.dtype == SP_DTYPE_FP8 || c.dtype == SP_DTYPE_INT8 ? 1 : 0;     // 8-bit copies of the four matrices
     ArenaLayout L{};
     size_t o = 0;
     auto take = [&](size_t bytes) { size_t at = o; o = align_up(o + bytes, 256); return at; };
@@ -121,6 +122,10 @@ WsLayout make_ws_layout(const sp_config& c, int total_tokens, int batch)
         W.attq = take(K * rows * H);
         W.gq = take(K * rows * F);
     }
+    if (c.dtype == SP_DTYPE_INT8 && rows >= (size_t)kFp8MinRows) {
+        W.codes = take(K * rows * (H > F ? H : F));
+        W.cscales = take(K * rows * 4);
+    }
     W.crows = (int)crows;
     W.end = o;
     W.rows = (int)rows;
@@ -191,6 +196,30 @@ static void quantize_transposed(uint8_t* dst8, float* scale, const float* src, s
         }
 }
 
+// code (o, i) = the 8-bit integer of src[i][o] in its output feature's row, as sp_quantize_int8 does it, [n_out][n_in]; src is [n_in][n_out]
+static void quantize_rows_transposed(int8_t* codes, float* scale, const float* src, size_t n_in, size_t n_out)
+{
+    std::vector<float> most(n_out, 0.f), factor(n_out);
+    for (size_t i = 0; i < n_in; ++i)
+        for (size_t o = 0; o < n_out; ++o) {
+            const float a = std::fabs(src[i * n_out + o]);
+            if (!(a <= most[o])) most[o] = std::isfinite(a) ? a : INFINITY;
+        }
+    for (size_t o = 0; o < n_out; ++o) {
+        const bool none = most[o] < 0x1p-100f, finite = std::isfinite(most[o]);
+        scale[o] = !finite ? std::nanf("") : none ? 0.f : most[o] / 127.f;
+        factor[o] = !finite || none ? 0.f : 127.f / most[o];
+    }
+    const size_t T = 32;
+    for (size_t i0 = 0; i0 < n_in; i0 += T)
+        for (size_t o0 = 0; o0 < n_out; o0 += T) {
+            const size_t i1 = i0 + T < n_in ? i0 + T : n_in, o1 = o0 + T < n_out ? o0 + T : n_out;
+            for (size_t o = o0; o < o1; ++o)
+                for (size_t i = i0; i < i1; ++i)
+                    codes[o * n_in + i] = factor[o] > 0.f ? (int8_t)std::nearbyint(src[i * n_out + o] * factor[o]) : (int8_t)0;
+        }
+}
+
 struct Writer {
     bool bf16;
     // copy n values as the arena's matrix element type
@@ -227,7 +256,11 @@ struct Writer {
 static void fill_student(const sp_config& c, const ArenaLayout& L, const float* src, char* dst)
 {
     const size_t H = c.hidden, F = c.ffn, C = c.classes, wb = bf16_path(c) ? 2 : 4;
-    const bool q8 = c.dtype == SP_DTYPE_FP8;
+    const bool fp8 = c.dtype == SP_DTYPE_FP8, int8 = c.dtype == SP_DTYPE_INT8;
+    auto eight_bits = [&](char* codes, char* scales, const float* m, size_t n_in, size_t n_out) {
+        if (fp8) quantize_transposed((uint8_t*)codes, (float*)scales, m, n_in, n_out);
+        if (int8) quantize_rows_transposed((int8_t*)codes, (float*)scales, m, n_in, n_out);
+    };
     Writer w{bf16_path(c)};
     const float* p = src;
     w.copy(dst + L.tok, p, (size_t)c.vocab * H); p += (size_t)c.vocab * H;
@@ -238,19 +271,19 @@ static void fill_student(const sp_config& c, const ArenaLayout& L, const float* 
         char* lb = dst + L.layer0 + (size_t)l * L.layer_stride;
         for (int part = 0; part < 3; ++part) {  // Wq bq Wk bk Wv bv -> rows [part*H, part*H+H) of the fused matrix
             if (part == 1) w.operand(lb + L.wk_io, p, H, H, H, 1);
-            if (q8) quantize_transposed((uint8_t*)(lb + L.wqkv8) + (size_t)part * H * H, (float*)(lb + L.sqkv) + part * H, p, H, H);
+            eight_bits(lb + L.wqkv8 + (size_t)part * H * H, lb + L.sqkv + (size_t)part * H * 4, p, H, H);
             w.transpose(lb + L.wqkv + (size_t)part * H * H * wb, p, H, H); p += H * H;
             memcpy(lb + L.bqkv + (size_t)part * H * 4, p, H * 4); p += H;
         }
-        if (q8) quantize_transposed((uint8_t*)(lb + L.wo8), (float*)(lb + L.so), p, H, H);
+        eight_bits(lb + L.wo8, lb + L.so, p, H, H);
         w.transpose(lb + L.wo, p, H, H); p += H * H;
         memcpy(lb + L.bo, p, H * 4); p += H;
         memcpy(lb + L.ln1g, p, H * 4); p += H;
         memcpy(lb + L.ln1b, p, H * 4); p += H;
-        if (q8) quantize_transposed((uint8_t*)(lb + L.w18), (float*)(lb + L.s1), p, H, F);
+        eight_bits(lb + L.w18, lb + L.s1, p, H, F);
         w.transpose(lb + L.w1, p, H, F); p += H * F;
         memcpy(lb + L.b1, p, F * 4); p += F;
-        if (q8) quantize_transposed((uint8_t*)(lb + L.w28), (float*)(lb + L.s2), p, F, H);
+        eight_bits(lb + L.w28, lb + L.s2, p, F, H);
         w.transpose(lb + L.w2, p, F, H); p += F * H;
         memcpy(lb + L.b2, p, H * 4); p += H;
         memcpy(lb + L.ln2g, p, H * 4); p += H;
@@ -301,6 +334,9 @@ static int run_students(const sp_model* M0, const WsLayout& W, const int32_t* id
     // quantised students: the four projections of the all-token layers on fp8 operands (large calls only)
     // (the fp8 kernel's tiles are 256 features wide: widths that are not multiples of it stay on the bf16 path)
     const bool fp8 = c.dtype == SP_DTYPE_FP8 && rows >= kFp8MinRows && W.xq && H % 256 == 0 && F % 256 == 0;
+    // ... or on 8-bit integers
+    const bool int8 = c.dtype == SP_DTYPE_INT8 && rows >= kFp8MinRows && W.codes;
+    const sp_attention_form* form = M0->has_form ? &M0->form : nullptr;
     // rows actually computed
     const int mtile = !bf16_path(c) ? 256 : 64;
     const int mrows = !bf16_path(c) && T <= 256 ? (T + (T > 64 ? 127 : 63)) / (T > 64 ? 128 : 64) * (T > 64 ? 128 : 64)
@@ -323,7 +359,7 @@ static int run_students(const sp_model* M0, const WsLayout& W, const int32_t* id
     // forwards of the tests unless they stop before the last layer.
     // Calls of fewer than kFirstOnlyMinTokens tokens have no compact buffers: their first-token rows use the q|k|v and FFN
     // buffers, which the folded layer leaves free, where those are large enough.
-    const bool first_only = !c.last_layer_all_tokens && with_head && attention_first_fold_supported(c, max_seqlen) &&
+    const bool first_only = !form && !c.last_layer_all_tokens && with_head && attention_first_fold_supported(c, max_seqlen) &&
                             (T >= kFirstOnlyMinTokens ||
                              ((size_t)B * c.heads <= (size_t)3 * rows && (size_t)B * c.heads * H <= (size_t)rows * F));
     const int crows = W.crows;
@@ -370,6 +406,45 @@ static int run_students(const sp_model* M0, const WsLayout& W, const int32_t* id
         }
         SP_MARK(SP_PHASE_LAYERNORM);
         return SP_OK;
+    };
+    // A projection of all token rows of students quantised in integers: the rows of src (width_in wide, student stride rows * width_in) to codes,
+    // and the product.  vt (not null): the fused q | k | v, its values transposed.
+    auto project_int8 = [&](const char* src, int width_in, size_t w_off, size_t s_off, size_t b_off, int N, int epilogue, const char* res, char* out,
+                            char* values) -> hipError_t {
+        const size_t most = H > F ? H : F;
+        int8_t* codes = (int8_t*)(w + W.codes) + (size_t)m0 * rows * most;
+        float* scales = (float*)(w + W.cscales) + (size_t)m0 * rows;
+        // (the padding rows of all students but the last are quantised with the others: nobody reads them)
+        const hipError_t e = launch_quantize_int8(src, width_in, SP_DTYPE_BF16, (k - 1) * rows + mrows, width_in, codes, width_in, width_in, scales, s);
+        if (e != hipSuccess) return e;
+        Int8Args a{};
+        a.A = codes; a.a_scales = scales; a.W = (const int8_t*)(M->arena + w_off); a.w_scales = (const float*)(M->arena + s_off);
+        a.bias = (const float*)(M->arena + b_off); a.res = res; a.out = out;
+        a.a_row = a.w_row = width_in; a.res_row = a.out_row = N;
+        a.a_ss = (size_t)rows * width_in; a.as_ss = (size_t)rows * 4; a.w_ss = a.ws_ss = a.b_ss = L.student_stride;
+        a.res_ss = a.out_ss = (size_t)rows * N * 2;
+        a.tokens = mrows; a.N = N; a.Kd = width_in; a.groups = k;
+        return values ? launch_gemm_int8_qkv(a, 2 * H, values, rows, sH, s) : launch_gemm_int8(a, SP_DTYPE_BF16, epilogue, s);
+    };
+    // Rotary positions on q and k of every token, in place, and the attention of the model's form
+    auto form_attention = [&]() -> hipError_t {
+        const int dtype = bf16_path(c) ? SP_DTYPE_BF16 : SP_DTYPE_FP32;
+        const int64_t row = 3 * H, all = (int64_t)rows * row;
+        if (form->rotary_dim) {
+            const hipError_t e = launch_rotary(qkv, row, 64, qkv, row, 64, dtype, T, 2 * c.heads, 64, form->rotary_dim, form->rotary_layout,
+                                               form->rotary_frequencies, form->rotary_factor, nullptr, cu, B, k, all, all, s);
+            if (e != hipSuccess) return e;
+        }
+        sp_attention_args a{};
+        a.q = qkv; a.k = qkv + H * ab; a.v = qkv + 2 * H * ab; a.out = att;
+        a.q_token = a.k_token = a.v_token = row; a.q_head = a.k_head = a.v_head = a.out_head = 64; a.out_token = H;
+        a.cu_q = a.cu_k = cu; a.dtype = dtype; a.batch = B; a.heads = a.kv_heads = c.heads; a.width = 64;
+        a.total_q = a.total_k = T; a.max_q = a.max_k = max_seqlen; a.scale = 0.125f; a.cap = form->cap; a.left = form->left; a.right = form->right;
+        a.reach = form->reach;
+        const int64_t table = (int64_t)c.heads * (2 * form->reach + 1);
+        if (form->slopes) a.slopes = form->slopes + (size_t)m0 * c.heads;
+        if (form->bias) a.bias = form->bias + (size_t)m0 * table;
+        return launch_attend(a, AttendGroups{k, all, all, all, (int64_t)rows * H, c.heads, table}, nullptr, s);
     };
     // g = gelu(LN(u; ln1) W1^T + b1) of n rows: fused while the rows of all students are few, else a LayerNorm launch and
     // the tile kernel
@@ -420,7 +495,7 @@ static int run_students(const sp_model* M0, const WsLayout& W, const int32_t* id
         SP_MARK(SP_PHASE_HEAD);
         return SP_OK;
     };
-    if (bf16_path(c) && T <= kRowsMaxTokens) {
+    if (bf16_path(c) && T <= kRowsMaxTokens && !form) {
         const size_t sT = (size_t)rows * H, sG = (size_t)rows * F, u_ss = part_ss;
         float *uo = small.o, *ud = small.d;
         // Many rows over all students: the tile kernel with a split reduction for the two projections onto the hidden width as
@@ -483,7 +558,7 @@ static int run_students(const sp_model* M0, const WsLayout& W, const int32_t* id
         return SP_OK;
     }
     // (the partial forwards of the tests read the buffers between the projections: not these either)
-    const bool f32_layer = with_head && f32_layer_supported(c, (long)T * k_rule);
+    const bool f32_layer = with_head && !form && f32_layer_supported(c, (long)T * k_rule);
     // Their rows' q|k|v alternate between two buffers: other workgroups read those of a layer while the next one's are written.  The last
     // layer's are in qkv.
     if (f32_layer && W.x1 - W.qkv2 < c.K * s3H) return SP_EINVAL;
@@ -493,7 +568,7 @@ static int run_students(const sp_model* M0, const WsLayout& W, const int32_t* id
     // eight launches a layer / embedding and q|k|v apart / in one, by tokens: one student 2718 82.5 / 73.8 / 75.2, 5475 93.1 / 78.7 / 78.7, 9143 98.0 / 82.7 /
     // 81.1, 14653 112.8 / 96.9 / 86.9; three 658 79.0 / 71.2 / 73.4, 2718 98.5 / 79.8 / 79.2, 5475 119.8 / 107.1 / 102.4, 9143 155.6 / 128.2 / 117.2, 14653 220.0 /
     // 175.1 / 166.0.
-    const bool narrow = with_head && !fp8 && layer_pays(c, (int64_t)T * k_rule);
+    const bool narrow = with_head && !fp8 && !int8 && !form && layer_pays(c, (int64_t)T * k_rule);
     const bool narrow_qkv = narrow && (int64_t)T * k_rule >= 8192 && !(first_only && c.layers == 1);
     if (narrow_qkv) SP_TRY(launch_embed_qkv(M, L.layer0, ids, cu, B, T, x, att, qkv, vt, rows, mrows, k, s));
     else if (f32_layer) SP_TRY(launch_f32_embed(M, L.layer0, ids, cu, B, T, x, f32_qkv(0), rows, k, s));
@@ -546,12 +621,14 @@ static int run_students(const sp_model* M0, const WsLayout& W, const int32_t* id
             return first_rows_tail(lo, f, att1, s1, false, !raw, x11, s1, g1, sg);
         }
         const bool left = f32_layer || (narrow_qkv && l == 0);          // the launch before has left q|k|v
-        if (fp8)
+        if (int8)
+            SP_TRY(project_int8(x, H, lo + L.wqkv8, lo + L.sqkv, lo + L.bqkv, 3 * H, SP_LINEAR_PLAIN, nullptr, qkv, form ? nullptr : vt));
+        else if (fp8)                                       // (with a form of attention the values stay with the others)
             SP_TRY(launch_gemm_fp8(M, xq, H, lo + L.wqkv8, lo + L.sqkv, lo + L.bqkv, kActQuantScale, qkv, 3 * H, nullptr, 0,
-                                   mrows, 3 * H, H, k, EPI_QKV, qH, s3H, 0, s, vt, 2 * H, rows, sH, 1.f));
+                                   mrows, 3 * H, H, k, EPI_QKV, qH, s3H, 0, s, vt, form ? 3 * H : 2 * H, rows, sH, 1.f));
         else if (bf16_path(c) && !left)
             SP_TRY(launch_gemm(M, x, H, lo + L.wqkv, lo + L.bqkv, qkv, 3 * H, nullptr, 0, mrows, 3 * H, H, k, EPI_QKV,
-                               sH, s3H, 0, s, vt, 2 * H, rows, sH));
+                               sH, s3H, 0, s, vt, form ? 3 * H : 2 * H, rows, sH));
         else if (!left)
             SP_TRY(launch_gemm(M, x, H, lo + L.wqkv, lo + L.bqkv, qkv, 3 * H, nullptr, 0, mrows, 3 * H, H, k, EPI_BIAS,
                                sH, s3H, 0, s));
@@ -571,15 +648,17 @@ static int run_students(const sp_model* M0, const WsLayout& W, const int32_t* id
         }
         // (quantised students: the output projection reads the fp8 copy only, so a whole forward skips the bf16 one;
         // the partial forwards of the tests keep it)
-        SP_TRY(launch_attention(M, qkv, vt, fp8 && with_head ? nullptr : att, cu, B, T, max_seqlen, rows, k, s, attq,
-                                kActQuantScale));
+        if (form) SP_TRY(form_attention());
+        else
+            SP_TRY(launch_attention(M, qkv, vt, fp8 && with_head ? nullptr : att, cu, B, T, max_seqlen, rows, k, s, attq,
+                                    kActQuantScale));
         SP_MARK(SP_PHASE_ATTENTION);
         if (narrow) {
             SP_TRY(launch_layer(M, lo, att, x, x, rows, mrows, k, s));
             SP_MARK(SP_PHASE_FFN_DOWN);
             continue;
         }
-        if (bf16_path(c) && !fp8) {
+        if (bf16_path(c) && !fp8 && !int8) {
             int rc = project_ln(att, H, sH, lo + L.wo, lo + L.bo, x, x1, lo + L.ln1g, lo + L.ln1b, SP_PHASE_OPROJ);
             if (rc != SP_OK) return rc;
             SP_TRY(launch_gemm(M, x1, H, lo + L.w1, lo + L.b1, g, F, nullptr, 0, mrows, F, H, k, EPI_BIAS_GELU, sH, sF, 0, s));
@@ -589,7 +668,8 @@ static int run_students(const sp_model* M0, const WsLayout& W, const int32_t* id
             if (rc != SP_OK) return rc;
             continue;
         }
-        if (fp8)
+        if (int8) SP_TRY(project_int8(att, H, lo + L.wo8, lo + L.so, lo + L.bo, H, SP_LINEAR_RESIDUAL, x, u, nullptr));
+        else if (fp8 && !form)
             SP_TRY(launch_gemm_fp8(M, attq, H, lo + L.wo8, lo + L.so, lo + L.bo, kActQuantScale, u, H, x, H, mrows, H, H, k,
                                    EPI_BIAS_RESIDUAL, qH, sH, sH, s, nullptr, 0, 0, 0, 1.f));
         else
@@ -597,14 +677,16 @@ static int run_students(const sp_model* M0, const WsLayout& W, const int32_t* id
         SP_MARK(SP_PHASE_OPROJ);
         SP_TRY(launch_layernorm(M, u, x1, rows, mrows, k, lo + L.ln1g, lo + L.ln1b, s, x1q, kActQuantScale));
         SP_MARK(SP_PHASE_LAYERNORM);
-        if (fp8)
+        if (int8) SP_TRY(project_int8(x1, H, lo + L.w18, lo + L.s1, lo + L.b1, F, SP_LINEAR_GELU, nullptr, g, nullptr));
+        else if (fp8)
             SP_TRY(launch_gemm_fp8(M, x1q, H, lo + L.w18, lo + L.s1, lo + L.b1, kActQuantScale, gq, F, nullptr, 0, mrows, F,
                                    H, k, EPI_BIAS_GELU, qH, qF, 0, s, nullptr, 0, 0, 0, kActQuantScale));
         else
             SP_TRY(launch_gemm(M, x1, H, lo + L.w1, lo + L.b1, g, F, nullptr, 0, mrows, F, H, k, EPI_BIAS_GELU, sH, sF, 0,
                                s));
         SP_MARK(SP_PHASE_FFN_UP);
-        if (fp8)
+        if (int8) SP_TRY(project_int8(g, F, lo + L.w28, lo + L.s2, lo + L.b2, H, SP_LINEAR_RESIDUAL, x1, u, nullptr));
+        else if (fp8)
             SP_TRY(launch_gemm_fp8(M, gq, F, lo + L.w28, lo + L.s2, lo + L.b2, kActQuantScale, u, H, x1, H, mrows, H, F, k,
                                    EPI_BIAS_RESIDUAL, qF, sH, sH, s, nullptr, 0, 0, 0, 1.f));
         else
@@ -912,6 +994,24 @@ int sp_probe_gelu_fp8(const float* x_device, float* y_device, int64_t n, void* h
     if (!x_device || !y_device) return SP_EINVAL;
     if (n < 1 || n > ((int64_t)1 << 31)) return SP_ESHAPE;
     return launch_gelu_q8_probe(x_device, y_device, (long)n, (hipStream_t)hip_stream) == hipSuccess ? SP_OK : SP_EHIP;
+}
+
+int sp_set_attention_form(sp_model* model, const sp_attention_form* form)
+{
+    if (!model) return SP_EINVAL;
+    if (!form) {
+        model->has_form = false;
+        return SP_OK;
+    }
+    if (form->rotary_dim < 0 || form->rotary_dim > 64 || form->rotary_dim % 2 || form->reach < 0 || form->reach > (1 << 20)) return SP_ESHAPE;
+    if (form->rotary_dim && (!form->rotary_frequencies || ((uintptr_t)form->rotary_frequencies & 7) || !std::isfinite(form->rotary_factor) ||
+                             (form->rotary_layout != SP_ROTARY_HALF && form->rotary_layout != SP_ROTARY_INTERLEAVED)))
+        return SP_EINVAL;
+    if (form->bias && (int64_t)model->cfg.K * model->cfg.heads * (2 * (int64_t)form->reach + 1) > (1 << 30)) return SP_ESHAPE;
+    if (!std::isfinite(form->cap) || ((uintptr_t)form->slopes & 3) || ((uintptr_t)form->bias & 3)) return SP_EINVAL;
+    model->form = *form;
+    model->has_form = true;
+    return SP_OK;
 }
 
 void sp_free(sp_model* model)

@@ -27,17 +27,14 @@ constexpr int kTablePad = 96;           // entries on each side of the table in 
 constexpr int kRun = 16;                // neighbouring workgroups that stay on one XCD
 constexpr int kTableBytes = 14336;      // largest table in LDS
 
-// cap tanh(scale s / cap) in base-2 units; cap2 = cap log2(e), pre = scale / cap (fp32) or 2 log2(e) scale / cap (bf16)
-template <class E>
-__device__ __forceinline__ float capped(float s, float pre, float cap2)
+// cap tanh(scale s / cap) in base-2 units, cap2 = cap log2(e), pre = 2 log2(e) scale / cap: tanh(y) = 1 - 2 / (e^(2 y) + 1), 2^-23 off in
+// absolute value, far inside what bf16 operands leave of a score.
+__device__ __forceinline__ float capped_far(float s, float pre, float cap2)
 {
-    if (sizeof(E) == 4) return cap2 * tanhf(s * pre);
-    // tanh(y) = 1 - 2 / (e^(2 y) + 1): 2^-23 off in absolute value, far inside what bf16 operands leave of a score
     return __builtin_fmaf(-2.f * cap2, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(s * pre) + 1.f), cap2);
 }
-
-// The same for |scale s / cap| < kNearCap, where five full-rate instructions do for two at a quarter of it and three more:
-// tanh(y) = y (1 + y^2 (a + y^2 (b + y^2 c))), coefficients in terms of s
+// The same for |scale s / cap| < kNearCap, where five full-rate instructions do for two at a quarter of it and three more, and where
+// fp32 needs it: tanh(y) = y (1 + y^2 (a + y^2 (b + y^2 c))), coefficients in terms of s
 constexpr float kNearCap = 0.4f;
 struct NearCap {
     float k0, k1, k2, k3;
@@ -53,12 +50,13 @@ struct AttendArgs {
     char* out;
     float* lse;
     size_t qt, qh, kh, vh, ot, oh;                          // strides in bytes
-    int kt, vt;
+    size_t qg, kg, vg, og;                                  // the same from group to group
+    int kt, vt, slopes_g, bias_g, groups;                   // (slopes, bias: elements)
     const int32_t *cu_q, *cu_k, *prefix, *q_first, *doc_q, *doc_k;
     const float *slopes, *bias;
     float *part, *part_ml;                                  // [splits][total_q * heads][DP] sums, and (maximum, sum) pairs
     // Scores in base-2 units: raw ones (nothing but a positive scale) are multiplied where the exponential is taken.  cap2: the cap; pre: see
-    // capped(); near_cap: |s| below which capped_near() does.
+    // capped_far(); near_cap: |s| below which capped_near() does.
     float mult, pre, cap2, near_cap;
     NearCap cap_near;
     int raw, batch, heads, kv_heads, share, width, total_q, total_k, max_q, max_k, left, right, reach;
@@ -111,16 +109,16 @@ struct Shape {
 };
 
 // Waves on a SIMD that the registers are shared out for.
-constexpr int waves_per_simd(bool b16, int dp, int kind)
+constexpr int waves_per_simd(bool b16, int dp, int kind, bool docs)
 {
-    return kind == kFew ? (!b16 && dp == 128 ? 1 : 2) : kind == kSmall ? (b16 && dp == 64 ? 4 : 2) : b16 && dp == 64 ? 3 : 2;
+    return !b16 && dp == 128 ? (kind == kMany && !docs ? 2 : 1) : b16 && dp == 64 && kind != kFew && !(docs && kind == kMany) ? 3 : 2;
 }
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 
-template <class E, int DP, int KIND>
-__global__ __launch_bounds__((Shape<E, DP, KIND>::WAVES * 64), waves_per_simd(sizeof(E) == 2, DP, KIND)) void attend_kernel(AttendArgs p)
+template <class E, int DP, int KIND, bool DOCS>
+__global__ __launch_bounds__((Shape<E, DP, KIND>::WAVES * 64), waves_per_simd(sizeof(E) == 2, DP, KIND, DOCS)) void attend_kernel(AttendArgs p)
 {
     using S = Shape<E, DP, KIND>;
     constexpr bool FEW = S::FEW;
@@ -130,10 +128,11 @@ __global__ __launch_bounds__((Shape<E, DP, KIND>::WAVES * 64), waves_per_simd(si
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), j31 = lane & 31, g = lane >> 5;
 
     // ---- which rows ----
-    int b, hk, r0, split, q0, nq, c0, c1;
+    int b, hk, m, r0, split, q0, nq, c0, c1;
     if (FEW) {
         b = blockIdx.x;
-        hk = blockIdx.y;
+        m = blockIdx.y / p.kv_heads;
+        hk = blockIdx.y - m * p.kv_heads;
         split = blockIdx.z;
         r0 = 0;
         c0 = p.cu_q[b];
@@ -142,12 +141,14 @@ __global__ __launch_bounds__((Shape<E, DP, KIND>::WAVES * 64), waves_per_simd(si
         // Neighbouring items of one key head read the same keys: runs of kRun stay on one XCD (workgroup id mod 8) and go round the XCDs,
         // another way each time, so that these have the same work whatever the lengths.  The last items come first: behind a causal
         // mask they are the longest, and what runs last should be short.
-        const int total = p.items * p.kv_heads * p.splits, y = (int)(gridDim.x >> 3) - 1 - (int)(blockIdx.x >> 3), round = y / kRun;
+        const int total = p.items * p.kv_heads * p.splits * p.groups, y = (int)(gridDim.x >> 3) - 1 - (int)(blockIdx.x >> 3), round = y / kRun;
         const int lin = (round * 8 + (((int)blockIdx.x + round) & 7)) * kRun + y % kRun;
         if (lin >= total) return;
         split = lin % p.splits;
         const int item = lin / p.splits % p.items;
         hk = lin / p.splits / p.items;
+        m = hk / p.kv_heads;
+        hk -= m * p.kv_heads;
         // Item i belongs to the last sequence with cu * share / ROWS + b <= i: every sequence gets as many as it has blocks of rows, at least
         b = last_sequence(p.cu_q, p.batch, lane, [&](int i, int c) { return ((int64_t)c * p.share >> SHIFT) + i <= item; }, c0, c1);
         const int64_t start = (int64_t)item - (((int64_t)c0 * p.share >> SHIFT) + b);
@@ -189,7 +190,7 @@ __global__ __launch_bounds__((Shape<E, DP, KIND>::WAVES * 64), waves_per_simd(si
     auto tile_start = [&](int t) { return (t < tiles1 ? t : t - tiles1 + from2) * KT; };
 
     // ---- queries, table ----
-    const char* qrow = p.q + (size_t)(q0 + query) * p.qt + (size_t)head * p.qh;
+    const char* qrow = p.q + m * p.qg + (size_t)(q0 + query) * p.qt + (size_t)head * p.qh;
     constexpr int QF = S::B16 ? DP / 16 : DP / 8;
     u32x4 qf[QF];                                           // bf16: dimensions 16 s + 8 g ..; fp32: 8 s + 4 g ..
 #pragma unroll
@@ -197,12 +198,12 @@ __global__ __launch_bounds__((Shape<E, DP, KIND>::WAVES * 64), waves_per_simd(si
         const int byte = (2 * s + g) * 16;
         qf[s] = byte < p.width * (int)sizeof(E) ? *(const u32x4*)(qrow + byte) : u32x4{0, 0, 0, 0};
     }
-    const int doc = p.doc_q ? p.doc_q[q0 + query] : 0;
-    const float slope = p.slopes ? p.slopes[head] * kLog2e : 0.f;
+    const int doc = DOCS ? p.doc_q[q0 + query] : 0;
+    const float slope = p.slopes ? p.slopes[m * p.slopes_g + head] * kLog2e : 0.f;
     float bias_left = 0.f, bias_right = 0.f;
     if (p.bias) {
-        bias_left = in_log2(p.bias[(size_t)head * (2 * p.reach + 1)]);
-        bias_right = in_log2(p.bias[(size_t)head * (2 * p.reach + 1) + 2 * p.reach]);
+        bias_left = in_log2(p.bias[(unsigned)(m * p.bias_g + head * (2 * p.reach + 1))]);
+        bias_right = in_log2(p.bias[(unsigned)(m * p.bias_g + head * (2 * p.reach + 1) + 2 * p.reach)]);
     }
     float* table = (float*)(lds + S::TABLE);
     const int pitch = 2 * (p.reach + kTablePad) + 1;
@@ -211,7 +212,7 @@ __global__ __launch_bounds__((Shape<E, DP, KIND>::WAVES * 64), waves_per_simd(si
     // ---- documents of the workgroup's rows ----
     int doc_lo = 0x7fffffff, doc_hi = -1;
     bool doc_one = true;                                    // all rows have the same one
-    if (p.doc_q && !FEW) {
+    if (DOCS && !FEW) {
         for (int x = r0 / p.share + lane; x <= re / p.share; x += 64) {
             const int d = p.doc_q[q0 + x];
             if (d >= 0) {
@@ -236,10 +237,10 @@ __global__ __launch_bounds__((Shape<E, DP, KIND>::WAVES * 64), waves_per_simd(si
     // zeros.  One register of address per lane for each of the two.
     const bool inside = fc * 16 < p.width * (int)sizeof(E);
     const int k_at = inside ? fr * p.kt + fc * 16 : INT32_MAX, v_at = inside ? fr * p.vt + fc * 16 : INT32_MAX;
-    const char* kbase = p.k + (size_t)k0 * p.kt + (size_t)hk * p.kh;
-    const char* vbase = p.v + (size_t)k0 * p.vt + (size_t)hk * p.vh;
+    const char* kbase = p.k + m * p.kg + (size_t)k0 * p.kt + (size_t)hk * p.kh;
+    const char* vbase = p.v + m * p.vg + (size_t)k0 * p.vt + (size_t)hk * p.vh;
     u32x4 kr[LPT], vr[LPT];
-    int dr[LPT], dk = 0;                                    // documents of the fetched rows; of the tile's key `ft`
+    int dr[LPT], dk = 0;                                    // documents of the fetched rows; of the tile's key `ft` (FEW: lane i has row i's)
     auto fetch = [&](int j0, bool docs) {
         const int last = n - j0 < KT ? n - j0 - 1 : KT - 1;
         const int kn = last * p.kt + p.width * (int)sizeof(E), vn = last * p.vt + p.width * (int)sizeof(E);
@@ -247,21 +248,21 @@ __global__ __launch_bounds__((Shape<E, DP, KIND>::WAVES * 64), waves_per_simd(si
         for (int i = 0; i < LPT; ++i) {
             kr[i] = load16_bounded(kbase + (size_t)j0 * p.kt, kn, k_at, i * RS * p.kt);
             vr[i] = load16_bounded(vbase + (size_t)j0 * p.vt, vn, v_at, i * RS * p.vt);
-            if (docs) {
+            if (DOCS && docs && !FEW) {
                 const int j = j0 + fr + i * RS;
                 dr[i] = p.doc_k[k0 + (j < n ? j : n - 1)];
             }
         }
-        if (docs && ft < KT) dk = p.doc_k[k0 + (j0 + ft < n ? j0 + ft : n - 1)];
+        if (DOCS && docs && ft < KT) dk = p.doc_k[k0 + (j0 + ft < n ? j0 + ft : n - 1)];
     };
     const int key_to = S::key_slot(fr, fc) * 16, value_to = S::TILE + S::value_slot(fr, fc) * 16;
     char* const mine = lds + (FEW ? wave * 2 * S::TILE : 0);
     auto put = [&](int j0, int buf, bool docs) {
         char* to = mine + (FEW ? 0 : buf * 2 * S::TILE);
-        if (docs) {                                         // values that no row sees become zeros: a weight of zero does not hide a NaN
+        if (DOCS && docs) {                                 // values that no row sees become zeros: a weight of zero does not hide a NaN
 #pragma unroll
             for (int i = 0; i < LPT; ++i)
-                if (dr[i] < 0) vr[i] = u32x4{0, 0, 0, 0};
+                if ((FEW ? __shfl(dk, fr + i * RS) : dr[i]) < 0) vr[i] = u32x4{0, 0, 0, 0};
         }
         int kto = key_to, vto = value_to;
         asm volatile("" : "+v"(kto), "+v"(vto));
@@ -271,18 +272,18 @@ __global__ __launch_bounds__((Shape<E, DP, KIND>::WAVES * 64), waves_per_simd(si
             *(u32x4*)(to + (kto ^ S::key_turn(i * RS) * 16) + i * step) = kr[i];
             *(u32x4*)(to + (vto ^ S::value_turn(i * RS) * 16) + i * step) = vr[i];
         }
-        if (docs && ft < KT) ((int*)(lds + S::DOCS))[(FEW ? wave : buf) * KT + ft] = dk;
+        if (DOCS && docs && ft < KT) ((int*)(lds + S::DOCS))[(FEW ? wave : buf) * KT + ft] = dk;
     };
 
-    // The first tile is requested before anything else is waited for.  (With documents it is not known yet.)
-    const bool ahead = !FEW && !p.doc_k && t_a < t_z;
+    // Short sequences: the first tile is requested before anything else is waited for.  (With documents it is not known yet.)
+    const bool ahead = KIND == kSmall && !DOCS && t_a < t_z;
     if (ahead) fetch(tile_start(t_a), false);
     if (!FEW && p.table) {
         for (int h = 0; h < p.share; ++h)
             for (int e = tid; e < pitch; e += S::NT) {
                 int d = e - kTablePad;
                 d = d < 0 ? 0 : d > 2 * p.reach ? 2 * p.reach : d;
-                table[h * pitch + e] = in_log2(p.bias[(size_t)(hk * p.share + h) * (2 * p.reach + 1) + d]);
+                table[h * pitch + e] = in_log2(p.bias[(unsigned)(m * p.bias_g + (hk * p.share + h) * (2 * p.reach + 1) + d)]);
             }
     }
 
@@ -316,6 +317,7 @@ __global__ __launch_bounds__((Shape<E, DP, KIND>::WAVES * 64), waves_per_simd(si
             for (int e = 0; e < 16; ++e) sc[nb][e] = 0.f;
 #pragma unroll
             for (int s = 0; s < QF; ++s) {
+                if (s % 4 == 0 && (s || nb)) __builtin_amdgcn_sched_barrier(0);     // (all fragments at once would not fit the registers)
                 const u32x4 a = *(const u32x4*)(tile + (kat ^ (s * 32)) + nb * 32 * RC * 16);
                 if constexpr (S::B16) {
                     sc[nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, qf[s]), sc[nb], 0, 0, 0);
@@ -333,16 +335,24 @@ __global__ __launch_bounds__((Shape<E, DP, KIND>::WAVES * 64), waves_per_simd(si
         const int jg = j0 + 4 * g;
         if (!raw) {
             if (p.cap2 > 0.f) {
-                float far = 0.f;
-                if (S::B16)
+                if constexpr (S::B16) {
+                    float far = 0.f;
 #pragma unroll
                     EACH_SCORE far = __builtin_fmaxf(far, __builtin_fabsf(sc[nb][v]));
-                if (S::B16 && __all(far < p.near_cap)) {
+                    if (__all(far < p.near_cap)) {
 #pragma unroll
-                    EACH_SCORE sc[nb][v] = capped_near(sc[nb][v], p.cap_near);
+                        EACH_SCORE sc[nb][v] = capped_near(sc[nb][v], p.cap_near);
+                    } else {
+#pragma unroll
+                        EACH_SCORE sc[nb][v] = capped_far(sc[nb][v], p.pre, p.cap2);
+                    }
                 } else {
 #pragma unroll
-                    EACH_SCORE sc[nb][v] = capped<E>(sc[nb][v], p.pre, p.cap2);
+                    EACH_SCORE {
+                        const float x = sc[nb][v], far = capped_far(x, p.pre, p.cap2);
+                        sc[nb][v] = __builtin_fabsf(x) < p.near_cap ? capped_near(x, p.cap_near) : far;
+                        if (v % 2) __builtin_amdgcn_sched_barrier(0);
+                    }
                 }
             } else {
 #pragma unroll
@@ -366,13 +376,13 @@ __global__ __launch_bounds__((Shape<E, DP, KIND>::WAVES * 64), waves_per_simd(si
                     EACH_SCORE sc[nb][v] += at[KEY_OFFSET];
                 } else {
                     // (32-bit offsets, few at a time: registers)
-                    const unsigned at = (unsigned)head * (unsigned)(2 * p.reach + 1) + (unsigned)p.reach;
+                    const unsigned at = (unsigned)(m * p.bias_g + head * (2 * p.reach + 1) + p.reach);
 #pragma unroll
                     EACH_SCORE {
                         int d = jg + KEY_OFFSET - pos;
                         d = d < -p.reach ? -p.reach : d > p.reach ? p.reach : d;
                         sc[nb][v] += in_log2(p.bias[at + (unsigned)d]);
-                        if (v % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+                        if (v % 2) __builtin_amdgcn_sched_barrier(0);
                     }
                 }
             }
@@ -382,7 +392,7 @@ __global__ __launch_bounds__((Shape<E, DP, KIND>::WAVES * 64), waves_per_simd(si
 #pragma unroll
             EACH_SCORE if (!((KEY_OFFSET >= a && KEY_OFFSET <= z) || KEY_OFFSET < pr)) sc[nb][v] = -INFINITY;
         }
-        if (doc_mask) {
+        if (DOCS && doc_mask) {
             const int* dt = (const int*)(lds + S::DOCS) + (FEW ? wave : buf) * KT + 4 * g;
 #pragma unroll
             EACH_SCORE { const int x = dt[KEY_OFFSET]; if (x != doc || x < 0) sc[nb][v] = -INFINITY; }
@@ -451,7 +461,7 @@ __global__ __launch_bounds__((Shape<E, DP, KIND>::WAVES * 64), waves_per_simd(si
     };
 
     if (FEW) {
-        const bool docs = p.doc_k != nullptr;
+        constexpr bool docs = DOCS;
         for (int t = t_a + wave; t < t_z; t += 4) {
             if (t == t_a + wave) fetch(tile_start(t), docs);
             put(tile_start(t), 0, docs);
@@ -467,7 +477,7 @@ __global__ __launch_bounds__((Shape<E, DP, KIND>::WAVES * 64), waves_per_simd(si
         for (int base = t_a; base < t_z; base += 64) {
             const int m = t_z - base < 64 ? t_z - base : 64;
             unsigned long long live = m == 64 ? ~0ull : (1ull << m) - 1, masked = 0;
-            if (p.doc_k) {
+            if constexpr (DOCS) {
                 // Four keys a lane, so that a load covers 256 of them; each wave looks at its share of the 64 tiles.  (Two places in LDS in turn:
                 // a wave is at most one barrier ahead.)
                 constexpr int LPK = KT / 4, TPL = 64 / LPK, OWN = 64 / S::WAVES;        // lanes of a tile, tiles of a load, tiles of a wave
@@ -482,12 +492,17 @@ __global__ __launch_bounds__((Shape<E, DP, KIND>::WAVES * 64), waves_per_simd(si
                         any = any || (d >= doc_lo && d <= doc_hi && j + e < n);
                         all = all && d == doc_lo && j + e < n;
                     }
-                    const unsigned long long some = __ballot(any), full = __ballot(all);
-                    constexpr unsigned long long one = (1ull << LPK) - 1;
+                    // (bit 0 of every group of LPK lanes: whether any of the group says so)
+                    unsigned long long some = __ballot(any), part = ~__ballot(all);
+#pragma unroll
+                    for (int x = LPK / 2; x; x >>= 1) {
+                        some |= some >> x;
+                        part |= part >> x;
+                    }
 #pragma unroll
                     for (int x = 0; x < TPL; ++x) {
-                        if (some >> x * LPK & one) l |= 1ull << (x0 + x);
-                        if ((full >> x * LPK & one) != one) u |= 1ull << (x0 + x);
+                        l |= (some >> x * LPK & 1) << (x0 + x);
+                        u |= (part >> x * LPK & 1) << (x0 + x);
                     }
                 }
                 unsigned long long* found = (unsigned long long*)(lds + S::FOUND) + (base - t_a >> 6 & 1) * 8;
@@ -562,7 +577,7 @@ __global__ __launch_bounds__((Shape<E, DP, KIND>::WAVES * 64), waves_per_simd(si
             sum += f[w] * ml[(w * 32 + row) * 2 + 1];
         }
         const int qu = row / p.share, he = hk * p.share + row - qu * p.share;
-        const size_t at = (size_t)(q0 + qu) * p.heads + he;
+        const size_t at = ((size_t)m * p.total_q + q0 + qu) * p.heads + he;
         const float inv = p.splits > 1 ? 1.f : sum > 0.f ? 1.f / sum : 0.f;
 #pragma unroll
         for (int i = 0; i < CPT; ++i) {
@@ -578,16 +593,16 @@ __global__ __launch_bounds__((Shape<E, DP, KIND>::WAVES * 64), waves_per_simd(si
 #pragma unroll
             for (int e = 0; e < 4; ++e) x[e] *= inv;
             if (p.splits > 1) {
-                *(f32x4*)(p.part + ((size_t)split * p.total_q * p.heads + at) * DP + c * 4) = x;
+                *(f32x4*)(p.part + ((size_t)split * p.groups * p.total_q * p.heads + at) * DP + c * 4) = x;
             } else {
-                E* out = (E*)(p.out + (size_t)(q0 + qu) * p.ot + (size_t)he * p.oh) + c * 4;
+                E* out = (E*)(p.out + m * p.og + (size_t)(q0 + qu) * p.ot + (size_t)he * p.oh) + c * 4;
                 if constexpr (S::B16) *(bf16x4*)out = bf16x4{(bf16)x[0], (bf16)x[1], (bf16)x[2], (bf16)x[3]};
                 else *(f32x4*)out = x;
             }
         }
         if (cc == 0) {
             if (p.splits > 1) {
-                float* to = p.part_ml + ((size_t)split * p.total_q * p.heads + at) * 2;
+                float* to = p.part_ml + ((size_t)split * p.groups * p.total_q * p.heads + at) * 2;
                 to[0] = top;
                 to[1] = sum;
             } else if (p.lse) {
@@ -596,10 +611,10 @@ __global__ __launch_bounds__((Shape<E, DP, KIND>::WAVES * 64), waves_per_simd(si
         }
         return;
     }
-    const size_t at = (size_t)(q0 + query) * p.heads + head;
+    const size_t at = ((size_t)m * p.total_q + q0 + query) * p.heads + head;
     if (p.splits > 1) {
         if (r >= rows) return;
-        const size_t row = (size_t)split * p.total_q * p.heads + at;
+        const size_t row = (size_t)split * p.groups * p.total_q * p.heads + at;
 #pragma unroll
         for (int d = 0; d < ND; ++d)
 #pragma unroll
@@ -638,7 +653,7 @@ __global__ __launch_bounds__((Shape<E, DP, KIND>::WAVES * 64), waves_per_simd(si
             const int row = x + lane / RC, rr = rw + row;
             if (rr >= rows) break;
             const int qu = rr / p.share, he = hk * p.share + rr - qu * p.share;
-            *(u32x4*)(p.out + (size_t)(q0 + qu) * p.ot + (size_t)he * p.oh + oc * 16) = *(const u32x4*)(stage + (row * RC + (oc ^ (RC == 8 ? row & 7 : row & 15))) * 16);
+            *(u32x4*)(p.out + m * p.og + (size_t)(q0 + qu) * p.ot + (size_t)he * p.oh + oc * 16) = *(const u32x4*)(stage + (row * RC + (oc ^ (RC == 8 ? row & 7 : row & 15))) * 16);
         }
 }
 
@@ -646,11 +661,11 @@ __global__ __launch_bounds__((Shape<E, DP, KIND>::WAVES * 64), waves_per_simd(si
 template <class E, int DP>
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs p)
 {
-    const int lane = threadIdx.x & 63, b = blockIdx.z, head = blockIdx.y, r = blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, b = blockIdx.z % p.batch, m = blockIdx.z / p.batch, head = blockIdx.y, r = blockIdx.x * 4 + (threadIdx.x >> 6);
     int q0, nq;
     sequence_range(p.cu_q[b], p.cu_q[b + 1], p.total_q, p.max_q, q0, nq);
     if (r >= nq) return;
-    const size_t step = (size_t)p.total_q * p.heads, at = (size_t)(q0 + r) * p.heads + head;
+    const size_t step = (size_t)p.groups * p.total_q * p.heads, at = ((size_t)m * p.total_q + q0 + r) * p.heads + head;
     float top = -INFINITY;
     for (int s = lane; s < p.splits; s += 64) top = __builtin_fmaxf(top, p.part_ml[(s * step + at) * 2]);
     top = wave_max(top);
@@ -664,7 +679,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs p)
         if (DP > 64) x1 += f * x[lane + 64];
     }
     const float inv = sum > 0.f ? 1.f / sum : 0.f;
-    E* out = (E*)(p.out + (size_t)(q0 + r) * p.ot + (size_t)head * p.oh);
+    E* out = (E*)(p.out + m * p.og + (size_t)(q0 + r) * p.ot + (size_t)head * p.oh);
     if (lane < p.width) out[lane] = (E)(x0 * inv);
     if (DP > 64 && lane + 64 < p.width) out[lane + 64] = (E)(x1 * inv);
     if (p.lse && lane == 0) p.lse[at] = sum > 0.f ? (top + __builtin_log2f(sum)) * kLn2 : -INFINITY;
@@ -678,7 +693,7 @@ struct Plan {
 // Shape of the workgroups: few rows where no sequence has more than 32, small where they have up to 96 on average (of 128 rows half
 // the waves would be idle).  Parts of a call: as many as give every compute unit two workgroups, of at least 256 keys for each wave (few
 // rows) or 512 for all of them.
-Plan make_plan(const sp_attention_args& a)
+Plan make_plan(const sp_attention_args& a, int groups, bool split)
 {
     Plan P{};
     const int share = a.heads / a.kv_heads;
@@ -686,24 +701,24 @@ Plan make_plan(const sp_attention_args& a)
     P.dp = a.width <= 64 ? 64 : 128;
     const int rows = P.kind == kMany ? 128 : 64;
     P.items = P.kind == kFew ? a.batch : (int)((int64_t)a.total_q * share / rows) + a.batch;
-    const int64_t blocks = P.kind == kFew ? (int64_t)a.batch * a.kv_heads : ((int64_t)a.max_q * share + rows - 1) / rows * a.batch * a.kv_heads;
+    const int64_t blocks = (P.kind == kFew ? (int64_t)a.batch : ((int64_t)a.max_q * share + rows - 1) / rows * a.batch) * a.kv_heads * groups;
     const int64_t want = (512 + blocks - 1) / blocks, most = a.max_k / (P.kind == kFew ? 1024 : 512);
     P.splits = (int)(want < most ? want : most);
-    P.splits = P.splits < 1 ? 1 : P.splits > 64 ? 64 : P.splits;
+    P.splits = P.splits < 1 || !split ? 1 : P.splits > 64 ? 64 : P.splits;
     if (P.splits > 1) {
-        const size_t rows = (size_t)P.splits * a.total_q * a.heads;
+        const size_t rows = (size_t)P.splits * groups * a.total_q * a.heads;
         P.part = rows * P.dp * 4;
         P.ml = rows * 8;
     }
     return P;
 }
 
-template <class E, int DP, int KIND>
+template <class E, int DP, int KIND, bool DOCS>
 hipError_t launch_shape(const AttendArgs& a, const Plan& P, hipStream_t s)
 {
     using S = Shape<E, DP, KIND>;
     const size_t smem = S::LDS + (!S::FEW && a.table ? (size_t)a.share * (2 * (a.reach + kTablePad) + 1) * 4 : 0);
-    auto kern = attend_kernel<E, DP, KIND>;
+    auto kern = attend_kernel<E, DP, KIND, DOCS>;
     static std::atomic<size_t> raised{0};                   // per instantiation; the attribute is sticky for the process
     if (smem > 48 * 1024 && raised.load(std::memory_order_acquire) < smem) {
         const size_t most = S::LDS + (S::FEW ? 0 : kTableBytes);
@@ -711,19 +726,25 @@ hipError_t launch_shape(const AttendArgs& a, const Plan& P, hipStream_t s)
         if (e != hipSuccess) return e;
         raised.store(most, std::memory_order_release);
     }
-    const dim3 grid = S::FEW ? dim3((unsigned)a.batch, (unsigned)a.kv_heads, (unsigned)P.splits)
-                          : dim3((unsigned)(((int64_t)P.items * a.kv_heads * P.splits + 8 * kRun - 1) / (8 * kRun) * (8 * kRun)));
+    const dim3 grid = S::FEW ? dim3((unsigned)a.batch, (unsigned)(a.kv_heads * a.groups), (unsigned)P.splits)
+                          : dim3((unsigned)(((int64_t)P.items * a.kv_heads * P.splits * a.groups + 8 * kRun - 1) / (8 * kRun) * (8 * kRun)));
     hipLaunchKernelGGL(kern, grid, dim3(S::WAVES * 64), smem, s, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || P.splits == 1) return e;
-    hipLaunchKernelGGL((attend_join_kernel<E, DP>), dim3((unsigned)((a.max_q + 3) / 4), (unsigned)a.heads, (unsigned)a.batch), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((attend_join_kernel<E, DP>), dim3((unsigned)((a.max_q + 3) / 4), (unsigned)a.heads, (unsigned)(a.batch * a.groups)), dim3(256), 0, s, a);
     return hipGetLastError();
+}
+
+template <class E, int DP, int KIND>
+hipError_t launch_docs(const AttendArgs& a, const Plan& P, hipStream_t s)
+{
+    return a.doc_k ? launch_shape<E, DP, KIND, true>(a, P, s) : launch_shape<E, DP, KIND, false>(a, P, s);
 }
 
 template <class E, int DP>
 hipError_t launch_kind(const AttendArgs& a, const Plan& P, hipStream_t s)
 {
-    return P.kind == kFew ? launch_shape<E, DP, kFew>(a, P, s) : P.kind == kSmall ? launch_shape<E, DP, kSmall>(a, P, s) : launch_shape<E, DP, kMany>(a, P, s);
+    return P.kind == kFew ? launch_docs<E, DP, kFew>(a, P, s) : P.kind == kSmall ? launch_docs<E, DP, kSmall>(a, P, s) : launch_docs<E, DP, kMany>(a, P, s);
 }
 
 template <class E>
@@ -736,13 +757,13 @@ hipError_t launch_type(const AttendArgs& a, const Plan& P, hipStream_t s)
 
 size_t attend_workspace_bytes(const sp_attention_args& a)
 {
-    const Plan P = make_plan(a);
+    const Plan P = make_plan(a, 1, true);
     return P.part + P.ml;
 }
 
-hipError_t launch_attend(const sp_attention_args& a, void* workspace, hipStream_t s)
+hipError_t launch_attend(const sp_attention_args& a, const AttendGroups& g, void* workspace, hipStream_t s)
 {
-    const Plan P = make_plan(a);
+    const Plan P = make_plan(a, g.groups, workspace != nullptr);
     const size_t sz = a.dtype == SP_DTYPE_FP32 ? 4 : 2;
     AttendArgs d{};
     d.q = (const char*)a.q; d.k = (const char*)a.k; d.v = (const char*)a.v; d.out = (char*)a.out; d.lse = a.lse;
@@ -755,13 +776,14 @@ hipError_t launch_attend(const sp_attention_args& a, void* workspace, hipStream_
     d.raw = !(a.cap > 0.f) && !a.slopes && !a.bias && a.scale > 0.f;
     d.mult = d.raw ? k0 : 1.f;
     d.cap2 = a.cap > 0.f ? a.cap * kLog2e : 0.f;
-    d.pre = a.cap > 0.f ? ratio * (sz == 2 ? 2.f * kLog2e : 1.f) : k0;
+    d.pre = a.cap > 0.f ? ratio * (2.f * kLog2e) : k0;
     d.near_cap = kNearCap / std::fabs(ratio);
     // (the least-squares fit of tanh(y) on |y| < 0.4, reweighted until its errors were even: 2.8e-8)
     d.cap_near = NearCap{k0, -0.33331388f * k0 * r2, 0.13268751f * k0 * r2 * r2, -0.04742304f * k0 * r2 * r2 * r2};
     d.batch = a.batch; d.heads = a.heads; d.kv_heads = a.kv_heads; d.share = a.heads / a.kv_heads; d.width = a.width;
     d.total_q = a.total_q; d.total_k = a.total_k; d.max_q = a.max_q; d.max_k = a.max_k; d.left = a.left; d.right = a.right; d.reach = a.reach;
-    d.items = P.items; d.splits = P.splits;
+    d.qg = g.q * sz; d.kg = g.k * sz; d.vg = g.v * sz; d.og = g.out * sz; d.slopes_g = a.slopes ? (int)g.slopes : 0; d.bias_g = a.bias ? (int)g.bias : 0;
+    d.groups = g.groups; d.items = P.items; d.splits = P.splits;
     d.table = a.bias && (int64_t)d.share * (2 * ((int64_t)a.reach + kTablePad) + 1) * 4 <= kTableBytes;
     return a.dtype == SP_DTYPE_FP32 ? launch_type<float>(d, P, s) : launch_type<bf16>(d, P, s);
 }
@@ -821,7 +843,7 @@ int sp_attention(const sp_attention_args* args, void* workspace, size_t workspac
     const size_t need = attend_workspace_bytes(*args);
     if (need && (!workspace || ((uintptr_t)workspace & 255))) return SP_EINVAL;
     if (workspace_bytes < need) return SP_ENOMEM;
-    return launch_attend(*args, workspace, (hipStream_t)hip_stream) == hipSuccess ? SP_OK : SP_EHIP;
+    return launch_attend(*args, AttendGroups{1, 0, 0, 0, 0, 0, 0}, need ? workspace : nullptr, (hipStream_t)hip_stream) == hipSuccess ? SP_OK : SP_EHIP;
 }
 
 }  // extern "C"

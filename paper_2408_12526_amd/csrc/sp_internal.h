@@ -12,8 +12,8 @@
 
 namespace sp {
 
-// SP_DTYPE_FP8 is the bf16 path with fp8 copies of the four projection matrices: everything that asks "bf16 or fp32
-// storage" treats the two alike.
+// SP_DTYPE_FP8 (SP_DTYPE_INT8) is the bf16 path with fp8 (8-bit integer) copies of the four projection matrices: everything that asks
+// "bf16 or fp32 storage" treats them alike.
 inline bool bf16_path(const sp_config& c) { return c.dtype != SP_DTYPE_FP32; }
 
 typedef __bf16 bf16;
@@ -234,7 +234,7 @@ struct ArenaLayout {
     // SP_DTYPE_FP8 only (0 otherwise), relative to the start of a layer: the fused q|k|v, attention-output, FFN-up and
     // FFN-down matrices once more as e4m3 codes and their per-output-feature scales (fp32).  Codes lie in blocks of 32
     // outputs x 64 inputs, [out / 32][in / 64][c % 2][c / 2][out % 32][in % 16] with c = in / 16 % 4: the two wave-loads of
-    // one matrix-instruction operand, 1 KB in a row each
+    // one matrix-instruction operand, 1 KB in a row each.  SP_DTYPE_INT8: the same matrices as 8-bit integers, [out][in]
     size_t wqkv8, sqkv, wo8, so, w18, s1, w28, s2;
     size_t wp, wp_t, bp, wc, bc;   // wp: [in][out] (column-parallel head kernel); wp_t: projection operand
     size_t student_stride;
@@ -250,6 +250,7 @@ struct WsLayout {
     size_t cqt, cxb;                     // folded queries / weighted mean rows: [K][crows][heads][H]
     size_t part;                         // fp32 rows between the few-row projections: [K][kRowsU][H]
     size_t lpart;                        // per-group logit sums when two groups of students run side by side: [2][B][C]
+    size_t codes, cscales;               // SP_DTYPE_INT8 only: a projection's input as integers, [K][rows][max(H, F)] bytes, and the rows' scales (fp32)
     size_t xq, x1q, attq, gq;            // SP_DTYPE_FP8 only: fp8 copies of x, x1 and att ([K][rows][H] bytes), fp8 g ([K][rows][F])
     int rows, crows;
     int act_bytes;
@@ -266,6 +267,8 @@ struct sp_model {
     hipStream_t aux = nullptr;
     hipEvent_t ev_fork = nullptr, ev_join = nullptr;
     std::mutex* mu = nullptr;
+    bool has_form = false;               // (sp_set_attention_form)
+    sp_attention_form form{};
 };
 
 namespace sp {

@@ -134,6 +134,8 @@ __global__ __launch_bounds__(256) void quantize_kernel(QuantArgs p)
 
 // ---- the product --------------------------------------------------------------------------------------------------
 
+constexpr int kEpiQkv = 3;                                  // see launch_gemm_int8_qkv
+
 // A result from its sum: (float)sum is off by half a step at most, as is every operation behind it.
 template <int EPI>
 __device__ __forceinline__ float finish(int sum, float scale, float bias, float res)
@@ -310,6 +312,7 @@ __global__ __launch_bounds__(256, TM * TN >= 16 ? 1 : 2) void gemm_int8_kernel(I
 #pragma unroll
                 for (int e = 0; e < 4; ++e) sum[c * 4 + e] = a[e];
             }
+            if (EPI == kEpiQkv && n >= p.n_split) continue;  // (n_split is a multiple of 8)
             E* to = out + tok * p.out_row + n;
             if (whole) {
                 Vec y;
@@ -321,6 +324,22 @@ __global__ __launch_bounds__(256, TM * TN >= 16 ? 1 : 2) void gemm_int8_kernel(I
 #pragma unroll
                 for (int e = 0; e < PER; ++e)
                     if (n + e < p.N) to[e] = (E)finish<EPI>(sum[e], st[q] * ws[e], bias[e], EPI == SP_LINEAR_RESIDUAL ? (float)from[e] : 0.f);
+            }
+        }
+        if constexpr (EPI == kEpiQkv) {
+            // channels of the value projection: a thread takes eight tokens of one, sixteen bytes of its row in vt
+            constexpr int TG = BM / 16;                     // groups of eight tokens in half a tile
+            for (int x = tid; x < BN * TG; x += 256) {
+                const int ch = x / TG, n1 = n0 + ch, t0 = x % TG * 8, tok = m0 + half * (BM / 2) + t0;
+                if (n1 < p.n_split || n1 >= p.N || tok >= p.tokens) continue;       // (tokens is a multiple of 8)
+                const float w1 = sw[n1], b1 = bs ? bs[n1] : 0.f;
+                bf16x8 y;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int t = t0 + e;
+                    y[e] = (bf16)finish<EPI>(stage[t * (BN / 4) + ((ch >> 2) ^ (t & SWZ))][ch & 3], sa[tok + e] * w1, b1, 0.f);
+                }
+                *(bf16x8*)((bf16*)((char*)p.vt + m * p.vt_ss) + (int64_t)(n1 - p.n_split) * p.ld_vt + tok) = y;
             }
         }
     }
@@ -462,11 +481,8 @@ hipError_t launch_few(const Int8Args& a, const QuantArgs& q, hipStream_t s)
 constexpr int kFewTokens = 64;
 
 template <class E, int EPI>
-hipError_t launch_epilogue(const Int8Args& a, hipStream_t s)
+hipError_t launch_tiles(const Int8Args& a, hipStream_t s)
 {
-    if (a.tokens <= 16) return launch_few<1, false, E, EPI>(a, QuantArgs{}, s);
-    if (a.tokens <= 32) return launch_few<2, false, E, EPI>(a, QuantArgs{}, s);
-    if (a.tokens <= kFewTokens) return launch_few<4, false, E, EPI>(a, QuantArgs{}, s);
     // Tile: rounds of tiles over the compute units, each at a price of so many us and so many for a k-tile of 64 codes (two workgroups of
     // the smaller ones share a unit, so that one's stores run while the other multiplies; the large one has it to itself).  us a call with the
     // quantiser, residual, tiles of 64 / 128 / 256 a side, by tokens: 4096 -> 1024 channels: 1024 23.5 / 33.7 / 65, 2048 30 / 36 / 66, 4096 51 / 42 / 72, 8192 93 / 73 /
@@ -480,6 +496,15 @@ hipError_t launch_epilogue(const Int8Args& a, hipStream_t s)
     const double c64 = cost(64, 2, 0.125), c128 = cost(128, 2, 0.33), c256 = cost(256, 10, 1);
     if (c256 <= c128 && c256 <= c64) return launch_tile<4, 4, E, EPI>(a, s);
     return c128 <= c64 ? launch_tile<2, 2, E, EPI>(a, s) : launch_tile<1, 1, E, EPI>(a, s);
+}
+
+template <class E, int EPI>
+hipError_t launch_epilogue(const Int8Args& a, hipStream_t s)
+{
+    if (a.tokens <= 16) return launch_few<1, false, E, EPI>(a, QuantArgs{}, s);
+    if (a.tokens <= 32) return launch_few<2, false, E, EPI>(a, QuantArgs{}, s);
+    if (a.tokens <= kFewTokens) return launch_few<4, false, E, EPI>(a, QuantArgs{}, s);
+    return launch_tiles<E, EPI>(a, s);
 }
 
 template <class E>
@@ -507,6 +532,16 @@ hipError_t launch_fused_type(const Int8Args& a, const QuantArgs& q, int epilogue
 hipError_t launch_gemm_int8(const Int8Args& a, int dtype, int epilogue, hipStream_t s)
 {
     return dtype == SP_DTYPE_FP32 ? launch_type<float>(a, epilogue, s) : launch_type<bf16>(a, epilogue, s);
+}
+
+hipError_t launch_gemm_int8_qkv(Int8Args a, int n_split, void* vt, int64_t ld_vt, size_t vt_ss, hipStream_t s)
+{
+    if (a.tokens % 8 || n_split % 8 || ld_vt % 8 || ((uintptr_t)vt & 15) || (vt_ss & 15)) return hipErrorInvalidValue;
+    a.n_split = n_split;
+    a.vt = vt;
+    a.ld_vt = ld_vt;
+    a.vt_ss = vt_ss;
+    return launch_tiles<bf16, kEpiQkv>(a, s);
 }
 
 static QuantArgs quant_args(const void* x, int64_t x_row, int dtype, int rows, int width, int8_t* codes, int64_t c_row, int padded, float* scales)

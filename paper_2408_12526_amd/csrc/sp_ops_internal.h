@@ -16,7 +16,7 @@ inline bool rows_apart(int64_t n0, int64_t s0, int64_t n1, int64_t s1, int64_t w
 
 hipError_t launch_rotary(const void* x, int64_t xt, int64_t xh, void* out, int64_t ot, int64_t oh, int dtype, int tokens,
                          int heads, int width, int dim, int layout, const double* freq, float factor, const int32_t* pos,
-                         const int32_t* cu, int batch, hipStream_t s);
+                         const int32_t* cu, int batch, int groups, int64_t xg, int64_t og, hipStream_t s);     // xg, og: elements from group to group
 
 // codes [rows][c_row]: `width` of them, then zeros up to `padded`
 hipError_t launch_quantize_int8(const void* x, int64_t x_row, int dtype, int rows, int width, int8_t* codes, int64_t c_row, int padded,
@@ -33,12 +33,25 @@ struct Int8Args {
     int64_t a_row, w_row, res_row, out_row;
     size_t a_ss, as_ss, w_ss, ws_ss, b_ss, res_ss, out_ss;      // bytes
     int tokens, N, Kd, groups;
+    void* vt;                           // see launch_gemm_int8_qkv
+    int64_t ld_vt;
+    size_t vt_ss;
+    int n_split;
 };
 bool linear_int8_fused(int tokens, int Kd);
 hipError_t launch_linear_int8_fused(const Int8Args& a, const void* x, int64_t x_row, int dtype, int epilogue, hipStream_t s);
 hipError_t launch_gemm_int8(const Int8Args& a, int dtype, int epilogue, hipStream_t s);
+// The fused q | k | v projection of students (bf16): bias; channels from n_split on are written transposed, vt[channel - n_split][token], ld_vt
+// tokens a row (a multiple of 8, at least `tokens`, which is one as well).
+hipError_t launch_gemm_int8_qkv(Int8Args a, int n_split, void* vt, int64_t ld_vt, size_t vt_ss, hipStream_t s);
 
+// `groups` students side by side: elements from one's q, k, v, out, slopes and bias to the next one's (their lse follow one another)
+struct AttendGroups {
+    int groups;
+    int64_t q, k, v, out, slopes, bias;
+};
 size_t attend_workspace_bytes(const sp_attention_args& a);
-hipError_t launch_attend(const sp_attention_args& a, void* workspace, hipStream_t s);
+// workspace null: never split over the keys
+hipError_t launch_attend(const sp_attention_args& a, const AttendGroups& g, void* workspace, hipStream_t s);
 
 }  // namespace sp

@@ -11,7 +11,7 @@ namespace {
 struct RotaryArgs {
     const char* x;
     char* out;
-    size_t xt, xh, ot, oh;              // strides in bytes
+    size_t xt, xh, ot, oh, xg, og;      // strides in bytes (token, head, group)
     const double* freq;
     const int32_t *pos, *cu;
     float factor;
@@ -44,8 +44,8 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs p)
         position = token - p.cu[lo];
     }
     const int h0 = blockIdx.y * p.per, h1 = h0 + p.per < p.heads ? h0 + p.per : p.heads;
-    const char* x = p.x + token * p.xt;
-    char* out = p.out + token * p.ot;
+    const char* x = p.x + token * p.xt + blockIdx.z * p.xg;
+    char* out = p.out + token * p.ot + blockIdx.z * p.og;
     if (u >= p.turn_units) {
         if (!p.copy) return;
         const int e0 = 2 * p.half + (u - p.turn_units) * 2 * V, n = p.width - e0 < 2 * V ? p.width - e0 : 2 * V;
@@ -99,17 +99,17 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs p)
 }
 
 template <class E, int V>
-hipError_t launch_width(RotaryArgs a, int layout, hipStream_t s)
+hipError_t launch_width(RotaryArgs a, int groups, int layout, hipStream_t s)
 {
     a.turn_units = a.half / V;
     a.units = a.turn_units + (a.copy ? (a.width - 2 * a.half + 2 * V - 1) / (2 * V) : 0);
     const long blocks = ((long)a.tokens * a.units + 255) / 256;
     // Heads of a thread: all of them share its sines, but a launch of few threads is spread over heads as well (four workgroups a
     // compute unit).
-    int groups = (int)(1024 / blocks);
-    groups = groups < 1 ? 1 : groups > a.heads ? a.heads : groups;
-    a.per = (a.heads + groups - 1) / groups;
-    const dim3 grid((unsigned)blocks, (unsigned)((a.heads + a.per - 1) / a.per));
+    int parts = (int)(1024 / (blocks * groups));
+    parts = parts < 1 ? 1 : parts > a.heads ? a.heads : parts;
+    a.per = (a.heads + parts - 1) / parts;
+    const dim3 grid((unsigned)blocks, (unsigned)((a.heads + a.per - 1) / a.per), (unsigned)groups);
     if (layout == SP_ROTARY_HALF) hipLaunchKernelGGL((rotary_kernel<E, V, SP_ROTARY_HALF>), grid, dim3(256), 0, s, a);
     else hipLaunchKernelGGL((rotary_kernel<E, V, SP_ROTARY_INTERLEAVED>), grid, dim3(256), 0, s, a);
     return hipGetLastError();
@@ -119,21 +119,22 @@ hipError_t launch_width(RotaryArgs a, int layout, hipStream_t s)
 
 hipError_t launch_rotary(const void* x, int64_t xt, int64_t xh, void* out, int64_t ot, int64_t oh, int dtype, int tokens,
                          int heads, int width, int dim, int layout, const double* freq, float factor, const int32_t* pos,
-                         const int32_t* cu, int batch, hipStream_t s)
+                         const int32_t* cu, int batch, int groups, int64_t xg, int64_t og, hipStream_t s)
 {
     const int sz = dtype == SP_DTYPE_FP32 ? 4 : 2;
-    const RotaryArgs a{(const char*)x, (char*)out, (size_t)(xt * sz), (size_t)(xh * sz), (size_t)(ot * sz), (size_t)(oh * sz), freq, pos, cu,
+    const RotaryArgs a{(const char*)x, (char*)out, (size_t)(xt * sz), (size_t)(xh * sz), (size_t)(ot * sz), (size_t)(oh * sz),
+                       (size_t)(xg * sz), (size_t)(og * sz), freq, pos, cu,
                        factor, tokens, heads, width, dim / 2, batch, 0, x != out && width > dim, 0, 0};
     // The widest pieces that every address is a multiple of
-    const size_t all = (size_t)x | (size_t)out | a.xt | a.xh | a.ot | a.oh | (size_t)(dim / 2 * sz);
+    const size_t all = (size_t)x | (size_t)out | a.xt | a.xh | a.ot | a.oh | a.xg | a.og | (size_t)(dim / 2 * sz);
     const int bytes = all % 16 == 0 ? 16 : all % 8 == 0 ? 8 : all % 4 == 0 ? 4 : 2;
     if (dtype == SP_DTYPE_FP32)
-        return bytes == 16 ? launch_width<float, 4>(a, layout, s) : bytes == 8 ? launch_width<float, 2>(a, layout, s) : launch_width<float, 1>(a, layout, s);
+        return bytes == 16 ? launch_width<float, 4>(a, groups, layout, s) : bytes == 8 ? launch_width<float, 2>(a, groups, layout, s) : launch_width<float, 1>(a, groups, layout, s);
     switch (bytes) {
-        case 16: return launch_width<bf16, 8>(a, layout, s);
-        case 8: return launch_width<bf16, 4>(a, layout, s);
-        case 4: return launch_width<bf16, 2>(a, layout, s);
-        default: return launch_width<bf16, 1>(a, layout, s);
+        case 16: return launch_width<bf16, 8>(a, groups, layout, s);
+        case 8: return launch_width<bf16, 4>(a, groups, layout, s);
+        case 4: return launch_width<bf16, 2>(a, groups, layout, s);
+        default: return launch_width<bf16, 1>(a, groups, layout, s);
     }
 }
 
@@ -184,7 +185,7 @@ int sp_rotary(const void* x, int64_t x_token, int64_t x_head, void* out, int64_t
     if (tokens == 0 || (cu_seqlens && batch == 0)) return SP_OK;
     if (!x || !out || ((uintptr_t)x & low) || ((uintptr_t)out & low)) return SP_EINVAL;
     return launch_rotary(x, x_token, x_head, out, out_token, out_head, dtype, tokens, heads, width, dim, layout, frequencies, factor,
-                         positions, cu_seqlens, batch, (hipStream_t)hip_stream) == hipSuccess ? SP_OK : SP_EHIP;
+                         positions, cu_seqlens, batch, 1, 0, 0, (hipStream_t)hip_stream) == hipSuccess ? SP_OK : SP_EHIP;
 }
 
 }  // extern "C"

@@ -16,7 +16,7 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libsp_mi355x.so")
 
-SP_DTYPE_FP32, SP_DTYPE_BF16, SP_DTYPE_FP8 = 0, 1, 2
+SP_DTYPE_FP32, SP_DTYPE_BF16, SP_DTYPE_FP8, SP_DTYPE_INT8 = 0, 1, 2, 3
 ACT_QUANT_SCALE = 16.0      # fp8 activations hold e4m3(16 * value)
 SP_BAD_ID, SP_BAD_CU0, SP_BAD_ORDER, SP_BAD_LENGTH, SP_BAD_TOTAL = 1, 2, 4, 8, 16
 PHASES = ("embed", "qkv", "attention", "oproj", "layernorm", "ffn_up", "ffn_down", "head", "last_first")
@@ -32,6 +32,11 @@ class sp_ws_layout(C.Structure):
     _fields_ = [(n, C.c_size_t) for n in ("x", "qkv", "vt", "att", "x1", "g", "z")] + [
         ("rows", C.c_int32), ("act_bytes", C.c_int32), ("first_q", C.c_size_t), ("first_att", C.c_size_t),
         ("first_rows", C.c_int32), ("xq", C.c_size_t), ("x1q", C.c_size_t), ("gq", C.c_size_t), ("attq", C.c_size_t)]
+
+
+class sp_attention_form(C.Structure):
+    _fields_ = [("rotary_dim", C.c_int32), ("rotary_layout", C.c_int32), ("rotary_frequencies", C.c_void_p), ("rotary_factor", C.c_float),
+                ("cap", C.c_float), ("left", C.c_int32), ("right", C.c_int32), ("slopes", C.c_void_p), ("bias", C.c_void_p), ("reach", C.c_int32)]
 
 
 def _load() -> C.CDLL:
@@ -59,6 +64,8 @@ def _load() -> C.CDLL:
     lib.sp_probe_e4m3.restype = C.c_int; lib.sp_probe_e4m3.argtypes = [vp, C.c_int64, vp]
     lib.sp_probe_mfma_rate.restype = C.c_int
     lib.sp_probe_mfma_rate.argtypes = [i32, i32, vp, vp, C.POINTER(C.c_float)]
+    lib.sp_set_attention_form.restype = C.c_int
+    lib.sp_set_attention_form.argtypes = [vp, C.POINTER(sp_attention_form)]
     lib.sp_free.restype = None; lib.sp_free.argtypes = [vp]
     lib.sp_strerror.restype = C.c_char_p; lib.sp_strerror.argtypes = [C.c_int]
     lib.sp_pack.restype = C.c_int; lib.sp_pack.argtypes = [vp, i32, vp]
@@ -86,7 +93,7 @@ def _check(rc: int) -> None:
 def make_config(K, layers, hidden, heads, ffn, vocab, max_pos, classes, dtype="bf16", ln_eps=1e-12,
                 last_layer_all_tokens=False, single_stream=False) -> sp_config:
     return sp_config(K, layers, hidden, heads, ffn, vocab, max_pos, classes,
-                     {"bf16": SP_DTYPE_BF16, "fp8": SP_DTYPE_FP8, "fp32": SP_DTYPE_FP32}[dtype], ln_eps, 1 if last_layer_all_tokens else 0,
+                     {"bf16": SP_DTYPE_BF16, "fp8": SP_DTYPE_FP8, "int8": SP_DTYPE_INT8, "fp32": SP_DTYPE_FP32}[dtype], ln_eps, 1 if last_layer_all_tokens else 0,
                      1 if single_stream else 0)
 
 
@@ -171,13 +178,15 @@ class Students:
         blob = np.ascontiguousarray(blob, dtype=np.float32)
         self.cfg = cfg
         self.device = torch.device(device)
+        if self.device.type == "cuda" and self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
         self.arena = torch.empty(sp_arena_bytes(cfg), dtype=torch.uint8, device=self.device)
         handle = C.c_void_p()
         with torch.cuda.device(self.device):
             _check(_lib.sp_load_students(C.byref(cfg), blob.ctypes.data, blob.size, self.arena.data_ptr(),
                                          self.arena.numel(), _stream_ptr(None), C.byref(handle)))
         self.handle = handle
-        self._ws = None
+        self._ws = self._form = None
 
     def workspace(self, total_tokens: int, batch: int) -> torch.Tensor:
         need = sp_workspace_bytes(self.cfg, total_tokens, batch)
@@ -188,6 +197,29 @@ class Students:
     def release_workspace(self) -> None:
         """Drop the cached workspace tensor (the next call that needs one allocates it again)."""
         self._ws = None
+
+    def set_attention_form(self, *, rotary_frequencies: torch.Tensor | None = None, rotary_layout: str = "half", rotary_factor: float = 1.0,
+                           cap: float = 0.0, window=None, slopes: torch.Tensor | None = None, bias: torch.Tensor | None = None) -> None:
+        """Rotary positions (frequencies: float64, see ops.rotary_frequencies), capped scores, a window (left, right) and biases by distance
+        (slopes: float32 [K, heads]; bias: float32 [K, heads, 2 reach + 1]) for the attention of every layer; without arguments the plain
+        form.  The tensors are kept until the form is replaced."""
+        K, A = self.cfg.K, self.cfg.heads
+        for t, dtype, shape in ((rotary_frequencies, torch.float64, None), (slopes, torch.float32, (K, A)), (bias, torch.float32, None)):
+            if t is not None and (t.dtype != dtype or t.device != self.device or not t.is_contiguous() or (shape and tuple(t.shape) != shape)):
+                raise ValueError(f"a contiguous {dtype} tensor on {self.device} is wanted" + (f" of shape {shape}" if shape else ""))
+        if rotary_frequencies is not None and rotary_frequencies.dim() != 1:
+            raise ValueError("rotary_frequencies: [rotated elements of a head / 2] is wanted")
+        if bias is not None and (bias.dim() != 3 or tuple(bias.shape[:2]) != (K, A) or bias.shape[2] % 2 == 0):
+            raise ValueError(f"bias: [{K}, {A}, 2 reach + 1] is wanted")
+        plain = rotary_frequencies is None and cap <= 0 and window is None and slopes is None and bias is None
+        left, right = (-1, -1) if window is None else window
+        form = sp_attention_form(
+            2 * rotary_frequencies.numel() if rotary_frequencies is not None else 0, {"half": 0, "interleaved": 1}[rotary_layout],
+            rotary_frequencies.data_ptr() if rotary_frequencies is not None else None, rotary_factor, cap, left, right,
+            slopes.data_ptr() if slopes is not None else None, bias.data_ptr() if bias is not None else None,
+            bias.shape[2] // 2 if bias is not None else 0)
+        _check(_lib.sp_set_attention_form(self.handle, None if plain else C.byref(form)))
+        self._form = None if plain else (rotary_frequencies, slopes, bias)
 
     def sp_forward(self, token_ids: torch.Tensor, cu_seqlens: torch.Tensor, max_seqlen: int, k_active: int,
                    logits_out: torch.Tensor | None = None, workspace: torch.Tensor | None = None, stream=None):
@@ -268,7 +300,7 @@ class Students:
         n = k_active * lay.rows * width
         t = ws[off:off + n * lay.act_bytes].view(dt).view(k_active, lay.rows, width)
         t = t[:, :total_tokens].double()
-        if name == "qkv" and lay.act_bytes == 2:      # bf16 mode keeps the values feature-major in `vt`
+        if name == "qkv" and lay.act_bytes == 2 and self._form is None:   # bf16 mode keeps the values feature-major in `vt`
             nv = k_active * H * lay.rows
             vt = ws[lay.vt:lay.vt + nv * 2].view(dt).view(k_active, H, lay.rows)
             t = t.clone()
