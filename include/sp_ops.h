@@ -43,7 +43,7 @@ int sp_quantize_int8(const void* x, int64_t x_row, int32_t dtype, int32_t rows, 
  *             stride residual_row; out may be residual with the same stride)
  *   workspace 256-byte aligned, >= sp_linear_int8_workspace_bytes(tokens, width_in)
  * tokens may be 0 (nothing is done); width_in is 1..131072, width_out at least 1.  A row with an infinity or a NaN gives a row of
- * NaN.  Errors: SP_EINVAL, SP_ESHAPE, SP_ENOMEM, SP_EHIP. */
+ * NaN.  GELU is within 4e-7 of the erf form.  Errors: SP_EINVAL, SP_ESHAPE (also: tokens beyond 2^28, w_row beyond 2^20), SP_ENOMEM, SP_EHIP. */
 enum { SP_LINEAR_PLAIN = 0, SP_LINEAR_GELU = 1, SP_LINEAR_RESIDUAL = 2 };
 size_t sp_linear_int8_workspace_bytes(int32_t tokens, int32_t width_in);
 int sp_linear_int8(const void* x, int64_t x_row, int32_t dtype, int32_t tokens, int32_t width_in, const int8_t* w_codes,
@@ -88,7 +88,7 @@ int sp_rotary(const void* x, int64_t x_token, int64_t x_head, void* out, int64_t
  *     s = scale q.k;   cap > 0: s = cap tanh(s / cap);   slopes: s -= slopes[h] |d|;   bias: s += bias[h][clip(d, -reach, reach) + reach]
  *     out = sum_j softmax_j(s) v_j,   lse = ln sum_j exp(s)          over the visible j
  * j is visible where (-left <= d <= right, a negative bound being none, or j < prefix[b]) and, with documents, doc_q = doc_k >= 0.
- * A bias of minus infinity hides a key too.  A query that sees nothing gets zeros and lse = minus infinity.  Sums and statistics are
+ * A bias of minus infinity hides a key too (finite ones below -2e38 weigh like -2e38); positions beyond +-2^30 count as that.  A query that sees nothing gets zeros and lse = minus infinity.  Sums and statistics are
  * fp32; bf16 rounds the probabilities to bf16 before their product with the values, and the result.
  * Keys behind a sequence's end and, with documents, keys of a negative document may hold anything; a visible key of one query must be
  * finite also where the mask hides it from another.
@@ -114,7 +114,8 @@ typedef struct {
 /* Workspace for a call with these sizes (contents of the arrays are not looked at); 0 where none is needed, and for malformed
  * arguments.  256-byte aligned; may be null where 0. */
 size_t sp_attention_workspace_bytes(const sp_attention_args* args);
-/* Errors: SP_EINVAL, SP_ESHAPE, SP_ENOMEM, SP_EHIP. */
+/* Errors: SP_EINVAL, SP_ESHAPE (also: batch beyond 65535, totals or strides beyond 2^29, token strides of k and v beyond 2^23, total_q *
+ * heads beyond 2^30, batch * heads beyond 2^24), SP_ENOMEM, SP_EHIP. */
 int sp_attention(const sp_attention_args* args, void* workspace, size_t workspace_bytes, void* hip_stream);
 
 #ifdef __cplusplus

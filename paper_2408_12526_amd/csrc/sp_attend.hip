@@ -63,11 +63,12 @@ struct AttendArgs {
     int items, splits, table;                               // table: whether the bias is in LDS
 };
 
-// Sixteen bytes per lane from base + soff (uniform) + voff, zeros from `bytes` on.
-__device__ __forceinline__ u32x4 load16_bounded(const char* base, int bytes, int voff, int soff)
+// Sixteen bytes per lane from base + off, zeros from `bytes` on.  (All of the offset is the lane's: the hardware's check of the bound goes
+// by that part.)
+__device__ __forceinline__ u32x4 load16_bounded(const char* base, int bytes, unsigned off)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
-    return __builtin_amdgcn_raw_buffer_load_b128(__builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), 0, bytes, 0x00020000), voff, soff, 0);
+    return __builtin_amdgcn_raw_buffer_load_b128(__builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), 0, bytes, 0x00020000), (int)off, 0, 0);
 #else
     return u32x4{};
 #endif
@@ -243,11 +244,13 @@ __global__ __launch_bounds__((Shape<E, DP, KIND>::WAVES * 64), waves_per_simd(si
     int dr[LPT], dk = 0;                                    // documents of the fetched rows; of the tile's key `ft` (FEW: lane i has row i's)
     auto fetch = [&](int j0, bool docs) {
         const int last = n - j0 < KT ? n - j0 - 1 : KT - 1;
+        unsigned ka = (unsigned)k_at, va = (unsigned)v_at;  // (opaque: the rows' offsets are formed anew, kept they would spill)
+        asm volatile("" : "+v"(ka), "+v"(va));
         const int kn = last * p.kt + p.width * (int)sizeof(E), vn = last * p.vt + p.width * (int)sizeof(E);
 #pragma unroll
         for (int i = 0; i < LPT; ++i) {
-            kr[i] = load16_bounded(kbase + (size_t)j0 * p.kt, kn, k_at, i * RS * p.kt);
-            vr[i] = load16_bounded(vbase + (size_t)j0 * p.vt, vn, v_at, i * RS * p.vt);
+            kr[i] = load16_bounded(kbase + (size_t)j0 * p.kt, kn, ka + (unsigned)(i * RS * p.kt));
+            vr[i] = load16_bounded(vbase + (size_t)j0 * p.vt, vn, va + (unsigned)(i * RS * p.vt));
             if (DOCS && docs && !FEW) {
                 const int j = j0 + fr + i * RS;
                 dr[i] = p.doc_k[k0 + (j < n ? j : n - 1)];
@@ -690,14 +693,16 @@ struct Plan {
     size_t part, ml;                    // bytes
 };
 
-// Shape of the workgroups: few rows where no sequence has more than 32, small where they have up to 96 on average (of 128 rows half
-// the waves would be idle).  Parts of a call: as many as give every compute unit two workgroups, of at least 256 keys for each wave (few
+// Shape of the workgroups: few rows where no sequence has more than 32, small where they have up to 96 (fp32, whose waves the matrix
+// products keep busy for longer: 192) on average, of 128 rows half the waves being idle then.  us a launch, small / many, width 64: fp32, 8
+// heads, 32 sequences of 158 on average 53 / 68, 2 of 2048 281 / 232; bf16, 16 heads, 64 sequences of 256 46 / 43, 4 of 4096 451 / 366; 12
+// heads, 256 sequences of 57 on average 41 / 57.  Parts of a call: as many as give every compute unit two workgroups, of at least 256 keys for each wave (few
 // rows) or 512 for all of them.
 Plan make_plan(const sp_attention_args& a, int groups, bool split)
 {
     Plan P{};
     const int share = a.heads / a.kv_heads;
-    P.kind = (int64_t)a.max_q * share <= kWaveRows ? kFew : (int64_t)a.total_q * share <= (int64_t)96 * a.batch ? kSmall : kMany;
+    P.kind = (int64_t)a.max_q * share <= kWaveRows ? kFew : (int64_t)a.total_q * share <= (int64_t)(a.dtype == SP_DTYPE_FP32 ? 192 : 96) * a.batch ? kSmall : kMany;
     P.dp = a.width <= 64 ? 64 : 128;
     const int rows = P.kind == kMany ? 128 : 64;
     P.items = P.kind == kFew ? a.batch : (int)((int64_t)a.total_q * share / rows) + a.batch;

@@ -51,7 +51,7 @@ struct QuantArgs {
     size_t c_row;
     float* scales;
     int rows, width, padded;
-    int x_wide, c_wide;                 // whether the rows of x, of the codes, are 16-byte aligned
+    int c_wide;                         // whether the rows of codes are 16-byte aligned
 };
 
 // A wave takes row `row`: units of 16 elements, lane after lane, kept in registers between the maximum and the codes up to R units a
@@ -60,12 +60,12 @@ template <class E, int R>
 __device__ __forceinline__ void quantize_row(const QuantArgs& p, int row, int8_t* c, int padded, float* scale_to)
 {
     constexpr int PER = 16 / sizeof(E);                     // elements of a 16-byte load
-    typedef E Vec __attribute__((ext_vector_type(PER)));
+    typedef E Vec __attribute__((ext_vector_type(PER), aligned(sizeof(E))));    // (rows may start anywhere: the hardware takes such loads)
     const int lane = threadIdx.x & 63;
     const E* x = (const E*)(p.x + row * p.x_row);
     const int units = (p.width + 15) >> 4;
     auto fetch = [&](int u, E (&v)[16]) {
-        if (p.x_wide && u * 16 + 16 <= p.width) {
+        if (u * 16 + 16 <= p.width) {
 #pragma unroll
             for (int i = 0; i < 16 / PER; ++i) {
                 const Vec w = ((const Vec*)(x + u * 16))[i];
@@ -147,7 +147,7 @@ __device__ __forceinline__ float finish(int sum, float scale, float bias, float 
 }
 
 struct Tile {
-    int mtiles, ntiles, total, group, wide;     // group: rows of tiles that are gone through together; wide: out and residual are 16-byte aligned
+    int mtiles, ntiles, total, group;   // group: rows of tiles that are gone through together
 };
 
 // A workgroup of 2 x 2 waves computes 64 TM tokens x 64 TN channels, a wave TM x TN blocks of 32 x 32 by v_mfma_i32_32x32x32_i8.  Both
@@ -265,7 +265,7 @@ __global__ __launch_bounds__(256, TM * TN >= 16 ? 1 : 2) void gemm_int8_kernel(I
     const E* res = (const E*)((const char*)p.res + m * p.res_ss);
     E* out = (E*)((char*)p.out + m * p.out_ss);
     constexpr int PER = 16 / sizeof(E), TPR = BN / PER, RPI = 256 / TPR, SWZ = BN / 4 < 32 ? BN / 4 - 1 : 31;
-    typedef E Vec __attribute__((ext_vector_type(PER)));
+    typedef E Vec __attribute__((ext_vector_type(PER), aligned(sizeof(E))));    // (rows may start anywhere)
     const int cc = tid % TPR, n = n0 + cc * PER;
     float ws[PER], bias[PER];
 #pragma unroll
@@ -275,7 +275,7 @@ __global__ __launch_bounds__(256, TM * TN >= 16 ? 1 : 2) void gemm_int8_kernel(I
     }
     v4i* stage = (v4i*)smem;
     constexpr int ITER = BM / 2 / RPI;
-    const bool whole = t.wide && n + PER <= p.N;
+    const bool whole = n + PER <= p.N;
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
         // scales and residual of all the thread's rows are requested before anything is waited for (rows behind the last repeat it)
@@ -364,7 +364,6 @@ hipError_t launch_tile(const Int8Args& a, hipStream_t s)
     t.ntiles = (a.N + 64 * TN - 1) / (64 * TN);
     t.total = t.mtiles * t.ntiles * a.groups;
     t.group = 16 / TM;                                      // (a thousand tokens)
-    t.wide = !(((uintptr_t)a.out | (uintptr_t)a.res | (size_t)(a.out_row * sizeof(E)) | (size_t)(a.res_row * sizeof(E)) | a.out_ss | a.res_ss) & 15);
     hipLaunchKernelGGL(kern, dim3((unsigned)((t.total + 7) / 8 * 8)), dim3(256), smem, s, a, t);
     return hipGetLastError();
 }
@@ -547,7 +546,7 @@ hipError_t launch_gemm_int8_qkv(Int8Args a, int n_split, void* vt, int64_t ld_vt
 static QuantArgs quant_args(const void* x, int64_t x_row, int dtype, int rows, int width, int8_t* codes, int64_t c_row, int padded, float* scales)
 {
     const size_t row = (size_t)(x_row * (dtype == SP_DTYPE_FP32 ? 4 : 2));
-    return QuantArgs{(const char*)x, row, codes, (size_t)c_row, scales, rows, width, padded, !(((uintptr_t)x | row) & 15),
+    return QuantArgs{(const char*)x, row, codes, (size_t)c_row, scales, rows, width, padded,
                      !(((uintptr_t)codes | (size_t)c_row) & 15)};
 }
 

@@ -19,6 +19,13 @@ struct RotaryArgs {
     int units, turn_units;              // units of a head: of V pairs, then of 2 V copied elements
 };
 
+// (the same instructions whatever V and layout, so that in place and not, and any alignment, give the same bits)
+__device__ __forceinline__ void turn(float a, float b, float c, float s, float& ra, float& rb)
+{
+    ra = __builtin_fmaf(a, c, -(b * s));
+    rb = __builtin_fmaf(b, c, a * s);
+}
+
 // One thread: V pairs (or 2 V elements behind the rotated ones) of one token, for `per` heads.  The angle is the same for every head:
 // its turns are formed in 64 bits, position * (frequency / 2 pi), and reduced there (2^-53 relative: 2^-33 turns off at
 // position 2^20), sine and cosine taken in fp32 from the fraction of a turn, once for all the thread's heads.
@@ -26,7 +33,7 @@ struct RotaryArgs {
 template <class E, int V, int LAYOUT>
 __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs p)
 {
-    typedef E Vec __attribute__((ext_vector_type(V)));
+    typedef E Vec __attribute__((ext_vector_type(V), aligned(sizeof(E))));      // (heads may start anywhere: the hardware takes such loads)
     const unsigned at = blockIdx.x * 256u + threadIdx.x;
     const int token = (int)(at / (unsigned)p.units), u = (int)(at - (unsigned)token * (unsigned)p.units);
     if (token >= p.tokens) return;
@@ -48,7 +55,9 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs p)
     char* out = p.out + token * p.ot + blockIdx.z * p.og;
     if (u >= p.turn_units) {
         if (!p.copy) return;
-        const int e0 = 2 * p.half + (u - p.turn_units) * 2 * V, n = p.width - e0 < 2 * V ? p.width - e0 : 2 * V;
+        int e0 = 2 * p.half + (u - p.turn_units) * 2 * V;
+        if (e0 + 2 * V > p.width && p.width - 2 * V >= 2 * p.half) e0 = p.width - 2 * V;    // (the last unit: some elements again)
+        const int n = p.width - e0 < 2 * V ? p.width - e0 : 2 * V;
         for (int h = h0; h < h1; ++h) {
             const E* a = (const E*)(x + h * p.xh) + e0;
             E* o = (E*)(out + h * p.oh) + e0;
@@ -62,17 +71,19 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs p)
         }
         return;
     }
+    // (the last unit of a head that is no multiple of V begins earlier and does some pairs again: never in place)
+    const int p0 = u * V + V <= p.half ? u * V : p.half - V;
     float cs[V], sn[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) {
-        double t = (double)position * (p.freq[u * V + e] * 0.15915494309189533577);    // 1 / 2 pi
+        double t = (double)position * (p.freq[p0 + e] * 0.15915494309189533577);    // 1 / 2 pi
         t -= __builtin_rint(t);
         float s, c;
         sincospif((float)(2.0 * t), &s, &c);
         cs[e] = c * p.factor;
         sn[e] = s * p.factor;
     }
-    const int ea = LAYOUT == SP_ROTARY_HALF ? u * V : 2 * u * V, eb = LAYOUT == SP_ROTARY_HALF ? p.half + u * V : ea + V;
+    const int ea = LAYOUT == SP_ROTARY_HALF ? p0 : 2 * p0, eb = LAYOUT == SP_ROTARY_HALF ? p.half + p0 : ea + V;
 #pragma unroll 4
     for (int h = h0; h < h1; ++h) {
         const Vec a = *(const Vec*)((const E*)(x + h * p.xh) + ea), b = *(const Vec*)((const E*)(x + h * p.xh) + eb);
@@ -80,17 +91,19 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs p)
 #pragma unroll
         for (int e = 0; e < V; ++e) {
             if (LAYOUT == SP_ROTARY_HALF) {
-                const float va = (float)a[e], vb = (float)b[e];
-                ra[e] = (E)(va * cs[e] - vb * sn[e]);
-                rb[e] = (E)(vb * cs[e] + va * sn[e]);
+                float r0, r1;
+                turn((float)a[e], (float)b[e], cs[e], sn[e], r0, r1);
+                ra[e] = (E)r0;
+                rb[e] = (E)r1;
             } else {                                        // pair e: elements 2 e and 2 e + 1 of the 2 V
                 const int i = 2 * e % V;
                 const float va = 2 * e < V ? (float)a[i] : (float)b[i], vb = 2 * e + 1 < V ? (float)a[(i + 1) % V] : (float)b[(i + 1) % V];
-                const E r0 = (E)(va * cs[e] - vb * sn[e]), r1 = (E)(vb * cs[e] + va * sn[e]);
-                if (2 * e < V) ra[i] = r0;
-                else rb[i] = r0;
-                if (2 * e + 1 < V) ra[(i + 1) % V] = r1;
-                else rb[(i + 1) % V] = r1;
+                float r0, r1;
+                turn(va, vb, cs[e], sn[e], r0, r1);
+                if (2 * e < V) ra[i] = (E)r0;
+                else rb[i] = (E)r0;
+                if (2 * e + 1 < V) ra[(i + 1) % V] = (E)r1;
+                else rb[(i + 1) % V] = (E)r1;
             }
         }
         *(Vec*)((E*)(out + h * p.oh) + ea) = ra;
@@ -101,7 +114,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs p)
 template <class E, int V>
 hipError_t launch_width(RotaryArgs a, int groups, int layout, hipStream_t s)
 {
-    a.turn_units = a.half / V;
+    a.turn_units = (a.half + V - 1) / V;
     a.units = a.turn_units + (a.copy ? (a.width - 2 * a.half + 2 * V - 1) / (2 * V) : 0);
     const long blocks = ((long)a.tokens * a.units + 255) / 256;
     // Heads of a thread: all of them share its sines, but a launch of few threads is spread over heads as well (four workgroups a
@@ -125,15 +138,15 @@ hipError_t launch_rotary(const void* x, int64_t xt, int64_t xh, void* out, int64
     const RotaryArgs a{(const char*)x, (char*)out, (size_t)(xt * sz), (size_t)(xh * sz), (size_t)(ot * sz), (size_t)(oh * sz),
                        (size_t)(xg * sz), (size_t)(og * sz), freq, pos, cu,
                        factor, tokens, heads, width, dim / 2, batch, 0, x != out && width > dim, 0, 0};
-    // The widest pieces that every address is a multiple of
-    const size_t all = (size_t)x | (size_t)out | a.xt | a.xh | a.ot | a.oh | a.xg | a.og | (size_t)(dim / 2 * sz);
-    const int bytes = all % 16 == 0 ? 16 : all % 8 == 0 ? 8 : all % 4 == 0 ? 4 : 2;
+    // Pairs of a unit: 16 bytes of each kind, fewer where the head has not as many, and in place where they do not divide it
+    int v = 16 / sz;
+    while (v > a.half || (x == out && a.half % v)) v >>= 1;
     if (dtype == SP_DTYPE_FP32)
-        return bytes == 16 ? launch_width<float, 4>(a, groups, layout, s) : bytes == 8 ? launch_width<float, 2>(a, groups, layout, s) : launch_width<float, 1>(a, groups, layout, s);
-    switch (bytes) {
-        case 16: return launch_width<bf16, 8>(a, groups, layout, s);
-        case 8: return launch_width<bf16, 4>(a, groups, layout, s);
-        case 4: return launch_width<bf16, 2>(a, groups, layout, s);
+        return v == 4 ? launch_width<float, 4>(a, groups, layout, s) : v == 2 ? launch_width<float, 2>(a, groups, layout, s) : launch_width<float, 1>(a, groups, layout, s);
+    switch (v) {
+        case 8: return launch_width<bf16, 8>(a, groups, layout, s);
+        case 4: return launch_width<bf16, 4>(a, groups, layout, s);
+        case 2: return launch_width<bf16, 2>(a, groups, layout, s);
         default: return launch_width<bf16, 1>(a, groups, layout, s);
     }
 }

@@ -327,6 +327,42 @@ def test_attention_long(dtype, nq, width):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("reach,heads,kv_heads", [(700, 2, 2), (3000, 4, 1), (300, 8, 1)])
+@pytest.mark.parametrize("n", [[50, 20], [300, 1]])
+def test_attention_tables_of_any_reach(dtype, reach, heads, kv_heads, n):
+    """Tables that fit the kernel's copy of them and tables that do not, distances on both sides of the reach."""
+    rng = np.random.default_rng(reach + heads)
+    q, k, v, cq, ck = batch_of(rng, dtype, n, n, heads, kv_heads, 64)
+    bias = rng.standard_normal((heads, 2 * reach + 1)).astype(np.float32)
+    check(dtype, q, k, v, cq, ck, bias=bias)
+    check(dtype, q, k, v, cq, ck, bias=bias, q_first=np.array([2 * reach, -reach], np.int32))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("width", [64, 128])
+def test_attention_documents_are_sequences(dtype, width):
+    """Documents of one long sequence (more key tiles than one look at them takes, not split over the keys) against the same rows as
+    sequences of their own: other tiles, so equal to the roundings of the type; causal, where the two are the same."""
+    rng = np.random.default_rng(15)
+    lengths = [1700, 3, 900, 64, 2400, 1]
+    n, A = sum(lengths), 16
+    cu = np.concatenate([[0], np.cumsum(lengths)]).astype(np.int32)
+    q, k, v = (dev(rng.standard_normal((n, A if i == 0 else 8, width)).astype(np.float32), dtype) for i in range(3))
+    doc = dev(np.repeat(np.arange(len(lengths)), lengths).astype(np.int32))
+    one = dev(np.array([0, n], np.int32))
+    want = ops.attention(q, k, v, dev(cu), 2400, causal=True, with_lse=True)
+    got = ops.attention(q, k, v, one, n, causal=True, doc_q=doc, with_lse=True)
+    # both are within the bound of the exact result that check() uses: weights and results rounded once each, values below 6
+    step = {"bf16": 2.0 ** -8, "fp32": 2.0 ** -18}[dtype]
+    assert (got[0].double() - want[0].double()).abs().max() <= 2 * 2 * step * float(v.float().abs().max())
+    assert (got[1] - want[1]).abs().max() <= 1e-4
+    apart = doc.clone()
+    apart[100:200] = -1
+    out, lse = ops.attention(q, k, v, one, n, doc_q=apart, with_lse=True)
+    assert bool((out[100:200] == 0).all()) and bool((lse[100:200] == -math.inf).all()) and bool(torch.isfinite(out).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("nq", [1, 40])
 def test_attention_unseen_keys_hold_anything(dtype, nq):
     """NaN and infinities in keys behind the sequences' ends, between them and in documents of negative number."""
