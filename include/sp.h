@@ -69,7 +69,8 @@ typedef struct {
                          projections' weights quantised at load with a scale per output feature, their inputs row by
                          row with a scale per token (the quantisation and the product are sp_quantize_int8 and
                          sp_linear_int8 of sp_ops.h); every activation also exists in bf16, and any widths that the bf16
-                         path takes will do. */
+                         path takes will do.  Nearer to bf16 than fp8 where a token has outliers, and slower than both: the
+                         inputs are quantised in passes of their own. */
     float ln_eps;     /* LayerNorm epsilon (BERT: 1e-12) */
     int32_t last_layer_all_tokens;
                       /* Only the first token of each sequence feeds the head (the pooled representation of
