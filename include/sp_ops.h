@@ -29,7 +29,7 @@ extern "C" {
  *
  * sp_quantize_int8: rows x [rows][width] (row stride x_row, at least width) -> codes [rows][width] (row stride
  * c_row, at least width) and scales [rows].  Codes behind `width` are left as they were.
- * Errors: SP_EINVAL, SP_ESHAPE, SP_EHIP. */
+ * Errors: SP_EINVAL, SP_ESHAPE (also: rows beyond 2^26 - 4), SP_EHIP. */
 int sp_quantize_int8(const void* x, int64_t x_row, int32_t dtype, int32_t rows, int32_t width, int8_t* codes,
                      int64_t c_row, float* scales, void* hip_stream);
 
@@ -43,7 +43,7 @@ int sp_quantize_int8(const void* x, int64_t x_row, int32_t dtype, int32_t rows, 
  *             stride residual_row; out may be residual with the same stride)
  *   workspace 256-byte aligned, >= sp_linear_int8_workspace_bytes(tokens, width_in)
  * tokens may be 0 (nothing is done); width_in is 1..131072, width_out at least 1.  A row with an infinity or a NaN gives a row of
- * NaN.  GELU is within 4e-7 of the erf form.  Errors: SP_EINVAL, SP_ESHAPE (also: tokens beyond 2^28, w_row beyond 2^20), SP_ENOMEM, SP_EHIP. */
+ * NaN.  GELU is within 4e-7 of the erf form.  Errors: SP_EINVAL, SP_ESHAPE (also: tokens beyond 2^26 - 4, w_row beyond 2^20), SP_ENOMEM, SP_EHIP. */
 enum { SP_LINEAR_PLAIN = 0, SP_LINEAR_GELU = 1, SP_LINEAR_RESIDUAL = 2 };
 size_t sp_linear_int8_workspace_bytes(int32_t tokens, int32_t width_in);
 int sp_linear_int8(const void* x, int64_t x_row, int32_t dtype, int32_t tokens, int32_t width_in, const int8_t* w_codes,
@@ -115,7 +115,7 @@ typedef struct {
  * arguments.  256-byte aligned; may be null where 0. */
 size_t sp_attention_workspace_bytes(const sp_attention_args* args);
 /* Errors: SP_EINVAL, SP_ESHAPE (also: batch beyond 65535, totals or strides beyond 2^29, token strides of k and v beyond 2^23, total_q *
- * heads beyond 2^30, batch * heads beyond 2^24), SP_ENOMEM, SP_EHIP. */
+ * heads beyond 2^30, batch * heads beyond 2^22), SP_ENOMEM, SP_EHIP. */
 int sp_attention(const sp_attention_args* args, void* workspace, size_t workspace_bytes, void* hip_stream);
 
 #ifdef __cplusplus

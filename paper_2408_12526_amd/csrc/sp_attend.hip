@@ -815,7 +815,7 @@ int check_attention(const sp_attention_args* a)
     if (a->width < 8 || a->width > 128 || a->width % 8) return SP_ESHAPE;
     constexpr int32_t most = 1 << 29;                      // (positions and distances stay inside 32 bits)
     if (a->batch > 65535 || a->total_q > most || a->total_k > most || a->total_q < 0 || a->total_k < 0 || a->max_q < 0 || a->max_k < 0) return SP_ESHAPE;
-    if ((int64_t)a->total_q * a->heads > (1 << 30) || (int64_t)a->batch * a->heads > (1 << 24)) return SP_ESHAPE;
+    if ((int64_t)a->total_q * a->heads > (1 << 30) || (int64_t)a->batch * a->heads > (1 << 22)) return SP_ESHAPE;
     if (!std::isfinite(a->scale) || !std::isfinite(a->cap) || a->reach < 0 || a->reach > (1 << 20)) return SP_EINVAL;
     if (a->bias && (int64_t)a->heads * (2 * (int64_t)a->reach + 1) > (1 << 30)) return SP_ESHAPE;
     if (!a->doc_q != !a->doc_k) return SP_EINVAL;

@@ -27,6 +27,7 @@ def linear(**k):
     (dict(epilogue=2, residual=4 * P, residual_row=9, out_row=8), EINVAL),
     (dict(tokens=-1), ESHAPE), (dict(width_in=0), ESHAPE), (dict(width_in=131073, w_row=131088), ESHAPE), (dict(width_out=0), ESHAPE),
     (dict(w_row=60), ESHAPE), (dict(w_row=72), ESHAPE), (dict(w_row=48), ESHAPE), (dict(out_row=7), ESHAPE), (dict(x_row=-64), ESHAPE),
+    (dict(tokens=1 << 26), ESHAPE), (dict(w_row=(1 << 20) + 16), ESHAPE),
     (dict(bytes=0), ENOMEM), (dict(bytes=4 * 128 + 15), ENOMEM),
 ])
 def test_linear_refuses(change, code):
@@ -47,6 +48,7 @@ def test_quantize_refuses():
     assert call(P, 8, 0, 2, 0, P, 8, P, None) == ESHAPE
     assert call(P, 8, 0, 2, 8, P, 7, P, None) == ESHAPE
     assert call(P, 8, 0, 0, 8, P, 8, P, None) == 0
+    assert call(P, 8, 0, 1 << 26, 8, P, 8, P, None) == ESHAPE
 
 
 def rotary(**k):
@@ -80,6 +82,8 @@ def attend(**k):
     (dict(cap=math.inf), EINVAL), (dict(reach=-1), EINVAL), (dict(q_token=132), EINVAL), (dict(out=P), EINVAL), (dict(out=2 * P), EINVAL),
     (dict(heads=3), ESHAPE), (dict(kv_heads=0), ESHAPE), (dict(width=4), ESHAPE), (dict(width=136), ESHAPE), (dict(width=60), ESHAPE),
     (dict(batch=-1), ESHAPE), (dict(total_q=-1), ESHAPE), (dict(max_k=-1), ESHAPE), (dict(out_head=0), ESHAPE), (dict(out_token=64), ESHAPE), (dict(k_token=-128), ESHAPE),
+    (dict(v_token=(1 << 23) + 8), ESHAPE), (dict(total_q=(1 << 29) + 1), ESHAPE), (dict(total_q=1 << 29, heads=4), ESHAPE), (dict(batch=65536), ESHAPE),
+    (dict(batch=65535, heads=128, kv_heads=128), ESHAPE), (dict(bias=7 * P, reach=1 << 20, heads=1024, kv_heads=1024), ESHAPE),
 ])
 def test_attention_refuses(change, code):
     assert attend(**change) == code
