@@ -186,9 +186,10 @@ int sp_forward_static(const sp_model* model, const int32_t* token_ids, const int
  * (scale 1/8, queries and keys of a sequence being the same tokens).  Null: back to the plain form.
  * The arrays are device memory of the caller, read by every forward until the form is replaced or the group freed.  Not to be called
  * while a call on the model is being issued by another thread; calls issued before keep the form they were issued with.
- * With a form every layer is computed for all tokens, in separate launches, whatever the size of the call (the learned position table of the
- * blob is still added: zeros there leave positions to the form); first-token rows, split sequences and fused layers are the plain
- * form's alone.  Quantised students (SP_DTYPE_FP8) compute the output projection in bf16.  The value slice of `qkv`
+ * With a form the layers run in separate launches, whatever the size of the call (the learned position table of the blob is still added: zeros there
+ * leave positions to the form); folded queries, split sequences and fused layers are the plain form's alone.  The last layer forms queries,
+ * keys and values of every token; in bf16 (and quantised) calls of up to 256 sequences what follows is computed for the first tokens only,
+ * in bf16, unless last_layer_all_tokens.  Quantised students (SP_DTYPE_FP8) compute the output projection in bf16.  The value slice of `qkv`
  * (sp_ws_layout) is written, `vt` is not.
  * Errors: SP_EINVAL (null or misaligned arrays, a cap that is not finite), SP_ESHAPE (rotary_dim odd or beyond 64, reach out of 0..2^20). */
 typedef struct {

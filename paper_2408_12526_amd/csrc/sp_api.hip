@@ -426,8 +426,8 @@ static int run_students(const sp_model* M0, const WsLayout& W, const int32_t* id
         a.tokens = mrows; a.N = N; a.Kd = width_in; a.groups = k;
         return values ? launch_gemm_int8_qkv(a, 2 * H, values, rows, sH, s) : launch_gemm_int8(a, SP_DTYPE_BF16, epilogue, s);
     };
-    // Rotary positions on q and k of every token, in place, and the attention of the model's form
-    auto form_attention = [&]() -> hipError_t {
+    // Rotary positions on q and k of every token, in place, and the attention of the model's form; first: of the first token of every sequence only
+    auto form_attention = [&](bool first) -> hipError_t {
         const int dtype = bf16_path(c) ? SP_DTYPE_BF16 : SP_DTYPE_FP32;
         const int64_t row = 3 * H, all = (int64_t)rows * row;
         if (form->rotary_dim) {
@@ -439,12 +439,12 @@ static int run_students(const sp_model* M0, const WsLayout& W, const int32_t* id
         a.q = qkv; a.k = qkv + H * ab; a.v = qkv + 2 * H * ab; a.out = att;
         a.q_token = a.k_token = a.v_token = row; a.q_head = a.k_head = a.v_head = a.out_head = 64; a.out_token = H;
         a.cu_q = a.cu_k = cu; a.dtype = dtype; a.batch = B; a.heads = a.kv_heads = c.heads; a.width = 64;
-        a.total_q = a.total_k = T; a.max_q = a.max_k = max_seqlen; a.scale = 0.125f; a.cap = form->cap; a.left = form->left; a.right = form->right;
+        a.total_q = a.total_k = T; a.max_q = first ? 1 : max_seqlen; a.max_k = max_seqlen; a.scale = 0.125f; a.cap = form->cap; a.left = form->left; a.right = form->right;
         a.reach = form->reach;
         const int64_t table = (int64_t)c.heads * (2 * form->reach + 1);
         if (form->slopes) a.slopes = form->slopes + (size_t)m0 * c.heads;
         if (form->bias) a.bias = form->bias + (size_t)m0 * table;
-        return launch_attend(a, AttendGroups{k, all, all, all, (int64_t)rows * H, c.heads, table}, nullptr, s);
+        return launch_attend(a, AttendGroups{k, all, all, all, (int64_t)rows * H, c.heads, table, true}, nullptr, s);
     };
     // g = gelu(LN(u; ln1) W1^T + b1) of n rows: fused while the rows of all students are few, else a LayerNorm launch and
     // the tile kernel
@@ -648,7 +648,15 @@ static int run_students(const sp_model* M0, const WsLayout& W, const int32_t* id
         }
         // (quantised students: the output projection reads the fp8 copy only, so a whole forward skips the bf16 one;
         // the partial forwards of the tests keep it)
-        if (form) SP_TRY(form_attention());
+        // With a form the last layer still forms q, k and v of every token (rotary keys cannot be folded into the queries); what follows is
+        // done for the first tokens only where their rows have a place.
+        if (form && l == c.layers - 1 && with_head && !c.last_layer_all_tokens && bf16_path(c) && B <= kRowsMaxTokens) {
+            SP_TRY(form_attention(true));
+            SP_MARK(SP_PHASE_LAST_FIRST);
+            const size_t sT = (size_t)rows * H;
+            return first_rows_tail(lo, small, (const bf16*)att, sT, true, true, (bf16*)x1, sT, (bf16*)g, (size_t)rows * F);
+        }
+        if (form) SP_TRY(form_attention(false));
         else
             SP_TRY(launch_attention(M, qkv, vt, fp8 && with_head ? nullptr : att, cu, B, T, max_seqlen, rows, k, s, attq,
                                     kActQuantScale));

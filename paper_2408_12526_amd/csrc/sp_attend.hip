@@ -66,7 +66,7 @@ struct AttendArgs {
     // capped_far(); near_cap: |s| below which capped_near() does.
     float mult, pre, cap2, near_cap;
     NearCap cap_near;
-    int raw, batch, heads, kv_heads, share, width, total_q, total_k, max_q, max_k, left, right, reach;
+    int from_start, raw, batch, heads, kv_heads, share, width, total_q, total_k, max_q, max_k, left, right, reach;
     int items, splits, table;                               // table: whether the bias is in LDS
 };
 
@@ -172,7 +172,7 @@ __global__ __launch_bounds__((Shape<E, DP, KIND>::WAVES * 64), waves_per_simd(si
         c1 = p.cu_k[b + 1];
     }
     sequence_range(c0, c1, p.total_k, p.max_k, k0, n);
-    int first = p.q_first ? p.q_first[b] : n - nq;
+    int first = p.q_first ? p.q_first[b] : p.from_start ? 0 : n - nq;
     first = first < -(1 << 30) ? -(1 << 30) : first > 1 << 30 ? 1 << 30 : first;
     int prefix = p.prefix ? p.prefix[b] : 0;
     prefix = prefix < 0 ? 0 : prefix > n ? n : prefix;
@@ -795,7 +795,7 @@ hipError_t launch_attend(const sp_attention_args& a, const AttendGroups& g, void
     d.batch = a.batch; d.heads = a.heads; d.kv_heads = a.kv_heads; d.share = a.heads / a.kv_heads; d.width = a.width;
     d.total_q = a.total_q; d.total_k = a.total_k; d.max_q = a.max_q; d.max_k = a.max_k; d.left = a.left; d.right = a.right; d.reach = a.reach;
     d.qg = g.q * sz; d.kg = g.k * sz; d.vg = g.v * sz; d.og = g.out * sz; d.slopes_g = a.slopes ? (int)g.slopes : 0; d.bias_g = a.bias ? (int)g.bias : 0;
-    d.groups = g.groups; d.items = P.items; d.splits = P.splits;
+    d.groups = g.groups; d.from_start = g.from_start; d.items = P.items; d.splits = P.splits;
     d.table = a.bias && (int64_t)d.share * (2 * ((int64_t)a.reach + kTablePad) + 1) * 4 <= kTableBytes;
     return a.dtype == SP_DTYPE_FP32 ? launch_type<float>(d, P, s) : launch_type<bf16>(d, P, s);
 }
@@ -855,7 +855,7 @@ int sp_attention(const sp_attention_args* args, void* workspace, size_t workspac
     const size_t need = attend_workspace_bytes(*args);
     if (need && (!workspace || ((uintptr_t)workspace & 255))) return SP_EINVAL;
     if (workspace_bytes < need) return SP_ENOMEM;
-    return launch_attend(*args, AttendGroups{1, 0, 0, 0, 0, 0, 0}, need ? workspace : nullptr, (hipStream_t)hip_stream) == hipSuccess ? SP_OK : SP_EHIP;
+    return launch_attend(*args, AttendGroups{1, 0, 0, 0, 0, 0, 0, false}, need ? workspace : nullptr, (hipStream_t)hip_stream) == hipSuccess ? SP_OK : SP_EHIP;
 }
 
 }  // extern "C"

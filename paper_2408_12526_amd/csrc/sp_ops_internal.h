@@ -49,6 +49,7 @@ hipError_t launch_gemm_int8_qkv(Int8Args a, int n_split, void* vt, int64_t ld_vt
 struct AttendGroups {
     int groups;
     int64_t q, k, v, out, slopes, bias;
+    bool from_start;                    // without q_first: the queries are the first of their sequence, not the last
 };
 size_t attend_workspace_bytes(const sp_attention_args& a);
 // workspace null: never split over the keys

@@ -25,9 +25,10 @@ def make(shape, lengths, seed=3):
     return blob, synth.make_ids(rng, int(lengths.sum()), shape.vocab), sp.sp_pack(lengths), int(lengths.max())
 
 
-def students_of(blob, shape, tokens=0, layers=None):
+def students_of(blob, shape, tokens=0, layers=None, first_only=False):
     """What the oracle consumes: the weights as the group keeps them, rounded to bf16, or in large calls of quantised students as 8-bit codes
-    times their scales (fp8 with a form of attention: all but the output projection)."""
+    times their scales (fp8 with a form of attention: all but the output projection; behind the last layer's attention the first tokens alone
+    are computed, in bf16, unless the group says otherwise)."""
     if shape.dtype == "fp32":
         return [synth.student_views(blob, shape, m) for m in range(shape.K)]
     w = torch.from_numpy(blob).bfloat16().float().numpy()
@@ -37,6 +38,8 @@ def students_of(blob, shape, tokens=0, layers=None):
             for name, x in views.items():
                 kind = name.split(".")[-1]
                 if layers is not None and not name.startswith(layers):
+                    continue
+                if first_only and name.startswith(f"l{shape.layers - 1}.") and kind in ("Wo", "W1", "W2"):
                     continue
                 if kind not in ("Wq", "Wk", "Wv", "Wo", "W1", "W2") or (shape.dtype == "fp8" and kind == "Wo"):
                     continue
@@ -84,13 +87,14 @@ def test_forms(dtype, which, size):
     shape = shape_of(dtype, hidden=256 if dtype == "fp8" else 128, ffn=512)
     blob, ids, cu, most = make(shape, LENGTHS[size])
     form = form_of(shape, which)
-    st = sp.Students(sp.config_from_shape(shape), blob)
+    whole = which in ("window", "all")                      # (the last layer for all tokens, else for the first ones only)
+    st = sp.Students(sp.config_from_shape(shape, last_layer_all_tokens=whole), blob)
     d_ids, d_cu = torch.from_numpy(ids).cuda(), torch.from_numpy(cu).cuda()
     plain = st.sp_forward(d_ids, d_cu, most, shape.K).clone()
     set_form(st, form)
     for k in (shape.K, 1) if size == "some" else (shape.K,):
         got = st.sp_forward(d_ids, d_cu, most, k).double().cpu().numpy()
-        args = students_of(blob, shape, len(ids)), shape.heads, shape.layers, shape.ln_eps, ids, cu, k
+        args = students_of(blob, shape, len(ids), first_only=not whole), shape.heads, shape.layers, shape.ln_eps, ids, cu, k
         want = sp_form_oracle.forward(*args, **form)
         tol = 1e-3 if dtype == "fp32" else sp_form_oracle.tolerance(want, dtype if len(ids) > 1792 else "bf16", *args, **form)
         assert np.abs(got - want).max() <= tol
