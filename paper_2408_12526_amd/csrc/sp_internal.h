@@ -40,7 +40,8 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 //     largest finite float as its upper bound: fminf / fmaxf, and a median with an infinite bound, which the
 //     compiler rewrites as one of them, cost a second instruction that quiets signalling NaNs first); |.| is an
 //     operand modifier.
-__device__ inline float gelu_erf_fast(float x)
+// positive: max(x, 0)
+__device__ inline float gelu_erf_from(float x, float positive)
 {
     const float a = __builtin_fabsf(__builtin_amdgcn_fmed3f(x, -6.0811f, 6.0811f));
     float q = __builtin_fmaf(2.992383634e-05f, a, -7.398715825e-04f);
@@ -49,8 +50,9 @@ __device__ inline float gelu_erf_fast(float x)
     q = __builtin_fmaf(q, a, -4.589156806e-01f);
     q = __builtin_fmaf(q, a, -1.151147127e+00f);
     const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(q, a, -1.0f));
-    return __builtin_fmaf(-a, e, __builtin_amdgcn_fmed3f(x, 0.0f, 3.402823466e+38f));
+    return __builtin_fmaf(-a, e, positive);
 }
+__device__ inline float gelu_erf_fast(float x) { return gelu_erf_from(x, __builtin_amdgcn_fmed3f(x, 0.0f, 3.402823466e+38f)); }
 
 // The same function where the result is stored as an e4m3 code (three mantissa bits: steps of 2^-4 relative): the
 // exponent is a cubic, log2(erfc(a / sqrt 2) / 2) ~ -1 + a (c0 + a (c1 + a c2)), fitted (minimax in the error of

@@ -136,12 +136,13 @@ __global__ __launch_bounds__(256) void quantize_kernel(QuantArgs p)
 
 constexpr int kEpiQkv = 3;                                  // see launch_gemm_int8_qkv
 
-// A result from its sum: (float)sum is off by half a step at most, as is every operation behind it.
+// A result from its sum: (float)sum is off by half a step at most, as is every operation behind it.  GELU keeps NaN (a scale of NaN is what the
+// quantiser makes of a row that holds one) and infinity: the maximum is the instruction that hands a NaN on, where a median of three drops it.
 template <int EPI>
 __device__ __forceinline__ float finish(int sum, float scale, float bias, float res)
 {
     float y = __builtin_fmaf((float)sum, scale, bias);
-    if (EPI == SP_LINEAR_GELU) y = gelu_erf_fast(y);
+    if (EPI == SP_LINEAR_GELU) y = gelu_erf_from(y, __builtin_elementwise_maximum(y, 0.f));
     if (EPI == SP_LINEAR_RESIDUAL) y += res;
     return y;
 }

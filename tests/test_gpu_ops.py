@@ -133,6 +133,36 @@ def test_linear_special_rows(tokens):
     near(got, want, bound)
 
 
+# The first token numbers reach the product's kernels for few tokens (fused, 32, 64), the last three its tiles of 64, 128 and 256.
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("how", ["plain", "gelu", "residual"])
+@pytest.mark.parametrize("tokens,width_out", [(4, 90), (20, 90), (40, 90), (100, 90), (1500, 2100), (4096, 4096)])
+def test_linear_carries_what_is_not_finite(dtype, how, tokens, width_out):
+    """Rows of x and of the weights with a NaN or an infinity are NaN under every epilogue; sums beyond the type are infinite, or
+    under GELU zero below."""
+    rng = np.random.default_rng(tokens)
+    K = 520
+    x = rng.standard_normal((tokens, K)).astype(np.float32)
+    x[0, 7], x[1, K - 1], x[tokens - 2, 0] = np.nan, np.inf, -np.inf
+    x[3] *= 1e30
+    x = dev(x, dtype)
+    w = rng.standard_normal((width_out, K)).astype(np.float32) * 0.05
+    w[5, 3], w[width_out - 1, 9] = np.nan, -np.inf
+    w[8::16] *= 1e12
+    w, ws = ops.quantize_int8(dev(w))
+    bias = rng.standard_normal(width_out).astype(np.float32)
+    res = dev(rng.standard_normal((tokens, width_out)).astype(np.float32), dtype) if how == "residual" else None
+    got = ops.linear_int8(x, w, ws, dev(bias), residual=res, gelu=how == "gelu")
+    some = np.unique([0, 1, 2, 3, tokens // 2, tokens - 2, tokens - 1])
+    want, bound = oracle.linear_int8(host(x)[some], w.cpu().numpy(), ws.cpu().numpy(), bias, None if res is None else host(res)[some], how == "gelu", dtype)
+    most = float(torch.finfo(TYPES[dtype]).max)
+    assert (np.abs(want[3]) > 1.01 * most).any() and not ((np.abs(want) > 0.99 * most) & (np.abs(want) < 1.01 * most)).any()
+    bound = np.where(np.isfinite(want) & (np.abs(want) <= most), bound, 0.0)
+    want = np.where(want > most, np.inf, np.where(want < -most, -np.inf, want))
+    assert np.isnan(want[[0, 1, -2]]).all() and np.isnan(want[:, [5, width_out - 1]]).all() and np.isnan(want).mean() < 0.8
+    near(got[some], want, bound, how)
+
+
 def test_linear_largest_depth():
     """The longest reduction, every code at its largest: the sum is 131072 * 127 * 127, just inside 32 bits."""
     K = 131072
