@@ -293,6 +293,6 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.Ten
     except (struct.error, OverflowError, TypeError) as e:
         raise ValueError(f"a size or number that does not fit its field: {e}") from None
     need = _lib.sp_attention_workspace_bytes(args)
-    ws = torch.empty(need, dtype=torch.uint8, device=q.device).data_ptr() if need else None
-    _call(dev, _lib.sp_attention, args, ws, need)
+    ws = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None      # (held until the launches are enqueued)
+    _call(dev, _lib.sp_attention, args, None if ws is None else ws.data_ptr(), need)
     return (out, lse) if with_lse else out

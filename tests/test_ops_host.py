@@ -1,6 +1,8 @@
 """The operators' C entries on the host: what they refuse before anything reaches a GPU, the frequencies, and the oracle's own pins."""
 import ctypes as C
+import gc
 import math
+import weakref
 
 import numpy as np
 import pytest
@@ -104,6 +106,36 @@ def test_no_cpu_path():
         ops.rotary(torch.ones(4, 2, 64), torch.ones(32, dtype=torch.float64), positions=torch.zeros(4, dtype=torch.int32))
     with pytest.raises(ValueError):
         ops.attention(*[torch.ones(4, 2, 64)] * 3, torch.tensor([0, 4], dtype=torch.int32), 4)
+
+
+def test_attention_holds_its_workspace_through_the_call(monkeypatch):
+    """Between a split call's two launches nobody else may be given the memory: its tensor lives until the call has returned."""
+    made, seen = [], []
+    empty = torch.empty
+
+    def remember(*a, **k):
+        t = empty(*a, **k)
+        made.append((weakref.ref(t), t.data_ptr()))
+        return t
+
+    class Library:
+        @staticmethod
+        def sp_attention_workspace_bytes(args):
+            return 4096
+
+        @staticmethod
+        def sp_attention(args, workspace, size, stream):
+            gc.collect()
+            seen.extend(r() is not None for r, at in made if at == workspace and r() is not None and r().numel() >= size == 4096)
+            return 0
+
+    monkeypatch.setattr(ops, "_home", lambda *a: 0)
+    monkeypatch.setattr(ops, "_call", lambda dev, fn, *a: fn(*a, None))
+    monkeypatch.setattr(ops, "_lib", Library)
+    monkeypatch.setattr(ops.torch, "empty", remember)
+    q, cu = torch.ones(4, 2, 64), torch.tensor([0, 4], dtype=torch.int32)
+    ops.attention(q, q.clone(), q.clone(), cu, 4)
+    assert seen == [True]
 
 
 # ---- frequencies ------------------------------------------------------------------------------------------------
