@@ -185,7 +185,8 @@ int sp_forward_static(const sp_model* model, const int32_t* token_ids, const int
  * positions, capped scores, a window, and biases by distance, as defined with sp_rotary and sp_attention in sp_ops.h
  * (scale 1/8, queries and keys of a sequence being the same tokens).  Null: back to the plain form.
  * The arrays are device memory of the caller, read by every forward until the form is replaced or the group freed.  Not to be called
- * while a call on the model is being issued by another thread; calls issued before keep the form they were issued with.
+ * while a call on the model is being issued by another thread; calls issued before keep the form they were issued with, and need its arrays until
+ * they are done: a call captured in a graph for as long as the graph is replayed.
  * With a form the layers run in separate launches, whatever the size of the call (the learned position table of the blob is still added: zeros there
  * leave positions to the form); folded queries, split sequences and fused layers are the plain form's alone.  The last layer forms queries,
  * keys and values of every token; in bf16 (and quantised) calls of up to 256 sequences what follows is computed for the first tokens only,

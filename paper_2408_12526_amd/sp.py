@@ -169,6 +169,13 @@ def _stream_ptr(stream) -> int:
     return int(s.cuda_stream)
 
 
+def _capturing(stream) -> bool:
+    if stream is None:
+        return torch.cuda.is_current_stream_capturing()
+    with torch.cuda.stream(stream):
+        return torch.cuda.is_current_stream_capturing()
+
+
 class Students:
     """A loaded student group: owns the device arena tensor and the library handle."""
 
@@ -187,6 +194,7 @@ class Students:
                                          self.arena.numel(), _stream_ptr(None), C.byref(handle)))
         self.handle = handle
         self._ws = self._form = None
+        self._form_streams, self._form_captured, self._kept_forms = set(), False, []      # (see _reads_form)
 
     def workspace(self, total_tokens: int, batch: int) -> torch.Tensor:
         need = sp_workspace_bytes(self.cfg, total_tokens, batch)
@@ -202,7 +210,8 @@ class Students:
                            cap: float = 0.0, window=None, slopes: torch.Tensor | None = None, bias: torch.Tensor | None = None) -> None:
         """Rotary positions (frequencies: float64, see ops.rotary_frequencies), capped scores, a window (left, right) and biases by distance
         (slopes: float32 [K, heads]; bias: float32 [K, heads, 2 reach + 1]) for the attention of every layer; without arguments the plain
-        form.  The tensors are kept until the form is replaced."""
+        form.  Calls issued before keep the form that they were issued with, and so do graphs: the tensors are held until the form is replaced and
+        the streams of its calls are done with them, or, once a call was captured in a graph, as long as this object lives."""
         K, A = self.cfg.K, self.cfg.heads
         for t, dtype, shape in ((rotary_frequencies, torch.float64, None), (slopes, torch.float32, (K, A)), (bias, torch.float32, None)):
             if t is not None and (t.dtype != dtype or t.device != self.device or not t.is_contiguous() or (shape and tuple(t.shape) != shape)):
@@ -219,7 +228,19 @@ class Students:
             slopes.data_ptr() if slopes is not None else None, bias.data_ptr() if bias is not None else None,
             bias.shape[2] // 2 if bias is not None else 0)
         _check(_lib.sp_set_attention_form(self.handle, None if plain else C.byref(form)))
-        self._form = None if plain else (rotary_frequencies, slopes, bias)
+        before, self._form = self._form, None if plain else [t for t in (rotary_frequencies, slopes, bias) if t is not None]
+        for t in before or ():
+            for s in self._form_streams:
+                t.record_stream(s)
+        if self._form_captured:
+            self._kept_forms.append(before)
+        self._form_streams, self._form_captured = set(), False
+
+    def _reads_form(self, stream) -> None:
+        """A call is about to be issued on `stream`: its kernels read the form's tensors there, those of a capture whenever it is replayed."""
+        if self._form is not None:
+            self._form_captured = self._form_captured or _capturing(stream)
+            self._form_streams.add(torch.cuda.current_stream() if stream is None else stream)
 
     def sp_forward(self, token_ids: torch.Tensor, cu_seqlens: torch.Tensor, max_seqlen: int, k_active: int,
                    logits_out: torch.Tensor | None = None, workspace: torch.Tensor | None = None, stream=None):
@@ -230,6 +251,7 @@ class Students:
         if logits_out is None:
             logits_out = torch.empty(batch, self.cfg.classes, dtype=torch.float32, device=self.device)
         ws = workspace if workspace is not None else self.workspace(total, batch)
+        self._reads_form(stream)
         _check(_lib.sp_forward(self.handle, token_ids.data_ptr(), cu_seqlens.data_ptr(), batch, total, max_seqlen,
                                k_active, ws.data_ptr(), ws.numel(), logits_out.data_ptr(), _stream_ptr(stream)))
         return logits_out
@@ -241,6 +263,7 @@ class Students:
         assert token_ids.is_cuda and cu_seqlens.is_cuda and token_ids.is_contiguous() and cu_seqlens.is_contiguous()
         assert logits_out.dtype == torch.float32 and logits_out.is_cuda and logits_out.is_contiguous()
         batch, total = cu_seqlens.numel() - 1, token_ids.numel()
+        self._reads_form(stream)
         _check(_lib.sp_forward_static(self.handle, token_ids.data_ptr(), cu_seqlens.data_ptr(), batch, total, max_seqlen,
                                       k_active, logits_out.data_ptr(), _stream_ptr(stream)))
         return logits_out
@@ -262,6 +285,7 @@ class Students:
             logits_out = torch.empty(batch, self.cfg.classes, dtype=torch.float32, device=self.device)
         ws = workspace if workspace is not None else self.workspace(total, batch)
         ms = (C.c_float * len(PHASES))()
+        self._reads_form(stream)
         _check(_lib.sp_forward_profiled(self.handle, token_ids.data_ptr(), cu_seqlens.data_ptr(), batch, total,
                                         max_seqlen, k_active, ws.data_ptr(), ws.numel(), logits_out.data_ptr(),
                                         _stream_ptr(stream), C.cast(ms, C.c_void_p)))
@@ -271,6 +295,7 @@ class Students:
                            stream=None):
         batch, total = cu_seqlens.numel() - 1, token_ids.numel()
         ws = workspace if workspace is not None else self.workspace(total, batch)
+        self._reads_form(stream)
         _check(_lib.sp_forward_partial(self.handle, token_ids.data_ptr(), cu_seqlens.data_ptr(), batch, total,
                                        max_seqlen, k_active, stop_after_layers, ws.data_ptr(), ws.numel(),
                                        _stream_ptr(stream)))

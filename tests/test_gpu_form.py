@@ -128,6 +128,60 @@ def test_form_in_two_groups_and_in_a_graph(dtype):
         assert torch.equal(out, want)
 
 
+def over(st, form):
+    """Replaces the form by nothing and writes NaN over whatever memory that gave back."""
+    st.set_attention_form()
+    sizes = {n: v.nbytes for n, v in form.items() if isinstance(v, np.ndarray)}
+    return [torch.full((size // 4,), float("nan"), device="cuda") for size in sizes.values() for _ in range(64)]
+
+
+@pytest.mark.parametrize("size", LENGTHS)
+def test_a_captured_call_keeps_its_form(size):
+    shape = shape_of("bf16")
+    blob, ids, cu, most = make(shape, LENGTHS[size])
+    form = form_of(shape, "all")
+    st = sp.Students(sp.config_from_shape(shape), blob)
+    d_ids, d_cu = torch.from_numpy(ids).cuda(), torch.from_numpy(cu).cuda()
+    set_form(st, form)
+    want = st.sp_forward(d_ids, d_cu, most, shape.K).clone()
+    out = torch.empty_like(want)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        st.sp_forward(d_ids, d_cu, most, shape.K, logits_out=out)
+    filled = over(st, form)
+    for _ in range(3):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+        st.sp_forward(d_ids, d_cu, most, shape.K)
+    assert len(filled) == 2 * 64
+
+
+def test_a_call_on_another_stream_keeps_its_form():
+    """The form is replaced, and its memory given out again, while a call that was issued with it still waits on its stream."""
+    shape = shape_of("bf16")
+    blob, ids, cu, most = make(shape, LENGTHS["some"])
+    form = form_of(shape, "all")
+    st = sp.Students(sp.config_from_shape(shape), blob)
+    d_ids, d_cu = torch.from_numpy(ids).cuda(), torch.from_numpy(cu).cuda()
+    set_form(st, form)
+    want = st.sp_forward(d_ids, d_cu, most, shape.K).clone()
+    a = torch.randn(8192, 8192, device="cuda")
+    ws = torch.empty_like(st.workspace(len(ids), len(cu) - 1))
+    out = torch.empty_like(want)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        for _ in range(8):                                  # (tens of milliseconds in front of the call)
+            a = a @ a
+    st.sp_forward(d_ids, d_cu, most, shape.K, logits_out=out, workspace=ws, stream=side)
+    filled = over(st, form)
+    torch.cuda.synchronize()
+    assert torch.equal(out, want) and len(filled) == 2 * 64
+
+
 @pytest.mark.parametrize("hidden,ffn", [(128, 384), (256, 512), (384, 640)])
 @pytest.mark.parametrize("with_form", [False, True])
 def test_int8_projections_stage_by_stage(hidden, ffn, with_form):
