@@ -88,7 +88,8 @@ int sp_rotary(const void* x, int64_t x_token, int64_t x_head, void* out, int64_t
  *     s = scale q.k;   cap > 0: s = cap tanh(s / cap);   slopes: s -= slopes[h] |d|;   bias: s += bias[h][clip(d, -reach, reach) + reach]
  *     out = sum_j softmax_j(s) v_j,   lse = ln sum_j exp(s)          over the visible j
  * j is visible where (-left <= d <= right, a negative bound being none, or j < prefix[b]) and, with documents, doc_q = doc_k >= 0.
- * A bias of minus infinity hides a key too (finite ones below -2e38 weigh like -2e38); positions beyond +-2^30 count as that.  A query that sees nothing gets zeros and lse = minus infinity.  Sums and statistics are
+ * A bias of minus infinity hides a key too (finite ones below -2e38 weigh like -2e38); positions beyond +-2^30 count as that.  A query
+ * that sees nothing gets zeros and lse = minus infinity; one that holds a NaN and sees a key gets NaN in both.  Sums and statistics are
  * fp32; bf16 rounds the probabilities to bf16 before their product with the values, and the result.
  * Keys behind a sequence's end and, with documents, keys of a negative document may hold anything; a visible key of one query must be
  * finite also where the mask hides it from another.

@@ -92,6 +92,9 @@ __device__ __forceinline__ void sequence_range(int t0, int t1, int total, int mo
 // A bias in units of the base-2 logarithm; finite ones stay finite.
 __device__ __forceinline__ float in_log2(float b) { return __builtin_isinf(b) ? b : __builtin_amdgcn_fmed3f(b * kLog2e, -3.0e38f, 3.0e38f); }
 
+// From a row's reference (base-2 units) and sum: zero where it has seen nothing, else one at least, or NaN, which stays NaN.
+__device__ __forceinline__ float lse_of(float top, float sum) { return sum == 0.f ? -INFINITY : (top + __builtin_log2f(sum)) * kLn2; }
+
 template <class E, int DP, int KIND>
 struct Shape {
     static constexpr bool B16 = sizeof(E) == 2, FEW = KIND == kFew;
@@ -616,7 +619,7 @@ __global__ __launch_bounds__((Shape<E, DP, KIND>::WAVES * 64), waves_per_simd(si
                 to[0] = top;
                 to[1] = sum;
             } else if (p.lse) {
-                p.lse[at] = sum > 0.f ? (top + __builtin_log2f(sum)) * kLn2 : -INFINITY;
+                p.lse[at] = lse_of(top, sum);
             }
         }
         return;
@@ -636,7 +639,7 @@ __global__ __launch_bounds__((Shape<E, DP, KIND>::WAVES * 64), waves_per_simd(si
         }
         return;
     }
-    if (g == 0 && r < rows && p.lse) p.lse[at] = lrun > 0.f ? (m2 + __builtin_log2f(lrun)) * kLn2 : -INFINITY;
+    if (g == 0 && r < rows && p.lse) p.lse[at] = lse_of(m2, lrun);
     barrier_lds();                                          // (the tiles are read no more)
     if (idle) return;
     // The wave's 32 rows leave through its quarter of the tiles as whole rows.
@@ -692,7 +695,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs p)
     E* out = (E*)(p.out + m * p.og + (size_t)(q0 + r) * p.ot + (size_t)head * p.oh);
     if (lane < p.width) out[lane] = (E)(x0 * inv);
     if (DP > 64 && lane + 64 < p.width) out[lane + 64] = (E)(x1 * inv);
-    if (p.lse && lane == 0) p.lse[at] = sum > 0.f ? (top + __builtin_log2f(sum)) * kLn2 : -INFINITY;
+    if (p.lse && lane == 0) p.lse[at] = lse_of(top, sum);
 }
 
 struct Plan {

@@ -414,6 +414,29 @@ def test_attention_unseen_keys_hold_anything(dtype, nq):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("how", [{}, dict(cap=3.0), dict(slopes=True)])
+@pytest.mark.parametrize("nq,nk", [([1, 2], [300, 1]), ([3, 5], [6000, 40]), ([40, 50], [40, 50]), ([300, 2], [300, 9])])
+def test_attention_queries_that_are_nan(dtype, how, nq, nk):
+    """A query with a NaN gets NaN in `out` and in lse, where minus infinity says that it saw nothing; its neighbours nothing of it."""
+    rng = np.random.default_rng(16)
+    q, k, v, cq, ck = batch_of(rng, dtype, nq, nk, 2, 1, 64)
+    how = dict(how, slopes=np.array([0.5, 0.25], np.float32)) if "slopes" in how else how
+    doc_k, doc_q = np.zeros(int(ck[-1]), np.int32), np.zeros(int(cq[-1]), np.int32)
+    doc_q[-1] = 1                                           # (the last query sees nothing)
+    for docs in ({}, dict(doc_q=doc_q, doc_k=doc_k)):
+        bad = q.clone()
+        bad[0, 1, 5] = bad[-1, 0, 0] = math.nan
+        want, wl, ob, lb = oracle.attention(host(q), host(k), host(v), cq, ck, dtype=dtype, **how, **docs)
+        want[0, 1], wl[0, 1] = math.nan, math.nan
+        if not docs:
+            want[-1, 0], wl[-1, 0] = math.nan, math.nan
+        t = {n: dev(x) if isinstance(x, np.ndarray) else x for n, x in {**how, **docs}.items()}
+        got, lse = ops.attention(bad, k, v, dev(cq), max(nq), dev(ck), max(nk), with_lse=True, **t)
+        near(got, want, ob, "out")
+        near(lse, wl, lb, "lse")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_attention_extreme_scores(dtype):
     """Scores so far apart that one key takes all, and scores near the lowest value of the type."""
     rng = np.random.default_rng(7)
