@@ -19,6 +19,7 @@
 // TB/s without it).  Short sequences: the chain from the offsets to the first tile and out again, about 8 us a workgroup: 256 sequences of 57 tokens on
 // average, 12 heads, 41 us.
 #include <atomic>
+#include <cfloat>
 #include <cmath>
 
 #include "sp_ops_internal.h"
@@ -791,10 +792,16 @@ hipError_t launch_attend(const sp_attention_args& a, const AttendGroups& g, void
     d.raw = !(a.cap > 0.f) && !a.slopes && !a.bias && a.scale > 0.f;
     d.mult = d.raw ? k0 : 1.f;
     d.cap2 = a.cap > 0.f ? a.cap * kLog2e : 0.f;
-    d.pre = a.cap > 0.f ? ratio * (2.f * kLog2e) : k0;
+    // (finite for the smallest cap as well: zero scores are multiplied by it)
+    d.pre = a.cap > 0.f ? std::fmin(std::fmax(ratio * (2.f * kLog2e), -FLT_MAX), FLT_MAX) : k0;
     d.near_cap = kNearCap / std::fabs(ratio);
     // (the least-squares fit of tanh(y) on |y| < 0.4, reweighted until its errors were even: 2.8e-8)
     d.cap_near = NearCap{k0, -0.33331388f * k0 * r2, 0.13268751f * k0 * r2 * r2, -0.04742304f * k0 * r2 * r2 * r2};
+    // A cap so small that the coefficients leave fp32: capped_far() alone, whose 2^-23 of that cap is nothing
+    if (!std::isfinite(d.cap_near.k3)) {
+        d.near_cap = 0.f;
+        d.cap_near = NearCap{};
+    }
     d.batch = a.batch; d.heads = a.heads; d.kv_heads = a.kv_heads; d.share = a.heads / a.kv_heads; d.width = a.width;
     d.total_q = a.total_q; d.total_k = a.total_k; d.max_q = a.max_q; d.max_k = a.max_k; d.left = a.left; d.right = a.right; d.reach = a.reach;
     d.qg = g.q * sz; d.kg = g.k * sz; d.vg = g.v * sz; d.og = g.out * sz; d.slopes_g = a.slopes ? (int)g.slopes : 0; d.bias_g = a.bias ? (int)g.bias : 0;

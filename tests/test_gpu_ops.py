@@ -437,6 +437,19 @@ def test_attention_queries_that_are_nan(dtype, how, nq, nk):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("cap", [1e-6, 3e-8, 1e-12, 1e-20, 1e-37, 1e-42, 1e20, 3e38])
+@pytest.mark.parametrize("nq", [1, 40])
+def test_attention_caps_of_any_size(dtype, cap, nq):
+    """Scores of exactly zero among others, where the cap is next to nothing or beyond everything."""
+    rng = np.random.default_rng(17)
+    q, k, v, cq, ck = batch_of(rng, dtype, [nq], [90], 2, 2, 64)
+    k[::3] = 0.0
+    q[0, 0] = 0.0
+    check(dtype, q, k, v, cq, ck, cap=float(np.float32(cap)))
+    check(dtype, q, k, v, cq, ck, cap=float(np.float32(cap)), scale=-2.0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_attention_extreme_scores(dtype):
     """Scores so far apart that one key takes all, and scores near the lowest value of the type."""
     rng = np.random.default_rng(7)
