@@ -14,7 +14,7 @@
 //
 // What bounds it: with many rows the vector instructions (a multiply-add, an exponential, a sum and half a maximum and conversion for a score: 28 cycles of
 // a SIMD; a cap 24 to 44 more) and the products, 32 cycles each, which overlap only between the two (width 64: three) waves that the registers leave a
-// SIMD.  bf16, 16 heads, 4 x 4096 tokens: width 128 on 4 key heads 650 us (840 TFLOP/s), causal 350, capped 760; width 64 366 (750), with slopes 514.
+// SIMD.  bf16, 16 heads, 4 x 4096 tokens: width 128 on 4 key heads 660 us (830 TFLOP/s), causal 359, capped 786; width 64 361 (760), with slopes 429.
 // With few rows the read of the keys and values: 8 queries of 32 heads on 4 key heads of 128 against 135 k keys, 270 MB, 65 us and 5 for the join (4.1
 // TB/s without it).  Short sequences: the chain from the offsets to the first tile and out again, about 8 us a workgroup: 256 sequences of 57 tokens on
 // average, 12 heads, 41 us.
@@ -419,9 +419,9 @@ __global__ __launch_bounds__((Shape<E, DP, KIND>::WAVES * 64), waves_per_simd(si
             swap_halves(l, h);
             mx = __builtin_fmaxf(l, h);
         }
-        // The reference of the exponentials moves where a row's maximum has outgrown it by 2^8, not with every new maximum (of 32 rows
-        // one has a new one in most tiles): weights up to 2^8 then, with the same relative rounding.
-        if (__any((mx - mrun) * mult > 8.f || (mrun == -INFINITY && mx > mrun))) {
+        // The reference of the exponentials is the maximum itself, so that the largest weight is one and bf16 does not round it.  (One that moves
+        // where it is outgrown by 2^8 only: 642 us for 660, causal 345 for 359, width 64 351 for 361, in the shapes above; short sequences the same.)
+        if (__any(mx > mrun)) {
             mx = __builtin_fmaxf(mx, mrun);
             const float alpha = mrun == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mrun - mx) * mult);
             mrun = mx;

@@ -461,6 +461,24 @@ def test_attention_extreme_scores(dtype):
     near(out[:, 0], host(v)[:, 0].astype(np.float64).mean(0)[None].repeat(50, 0), np.full((50, 64), 2.0 ** -7 * np.abs(host(v)).max()))
 
 
+@pytest.mark.parametrize("width", [64, 128])
+@pytest.mark.parametrize("nq,n,heads", [(4, 700, 2), (16, 3000, 1), (60, 300, 2), (300, 300, 2), (1000, 700, 2)])
+@pytest.mark.parametrize("how", [{}, dict(cap=1000.0)])
+def test_attention_largest_weight_is_one(width, nq, n, heads, how):
+    """A key far back that outgrows the others by less than the exponent of a few bits: its weight, of which bf16 has half a step otherwise, is
+    exactly one, so its value goes into the result with the roundings of fp32 and of the result alone."""
+    rng = np.random.default_rng(19)
+    q, k, v, cq, ck = batch_of(rng, "bf16", [nq], [n], heads, heads, width)
+    q.zero_(), k.zero_(), v.zero_()
+    q[:, :, 0] = dev(rng.uniform(0.1, 5.5, (nq, heads)).astype(np.float32), "bf16")
+    k[n - 7, :, 0] = 1.0
+    v[n - 7] = dev(rng.standard_normal((heads, width)).astype(np.float32), "bf16")
+    got = ops.attention(q, k, v, dev(cq), nq, dev(ck), n, scale=1.0, **how)
+    want, _, ob, _ = oracle.attention(host(q), host(k), host(v), cq, ck, scale=1.0, dtype="bf16", **how)
+    # (the oracle's bound holds a half step for the weights: all but one of them stand before values of zero)
+    near(got, want, ob - 2.0 ** -8 * np.abs(want))
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_attention_views(dtype):
     """q, k and v inside one buffer of q | k | v rows; heads in front of tokens; the output inside a wider one."""
