@@ -29,7 +29,7 @@ extern "C" {
  *
  * sp_quantize_int8: rows x [rows][width] (row stride x_row, at least width) -> codes [rows][width] (row stride
  * c_row, at least width) and scales [rows].  Codes behind `width` are left as they were.
- * Errors: SP_EINVAL, SP_ESHAPE (also: rows beyond 2^26 - 4), SP_EHIP. */
+ * Errors: SP_EINVAL, SP_ESHAPE (also: rows beyond 2^26 - 4, width beyond 2^31 - 2049), SP_EHIP. */
 int sp_quantize_int8(const void* x, int64_t x_row, int32_t dtype, int32_t rows, int32_t width, int8_t* codes,
                      int64_t c_row, float* scales, void* hip_stream);
 

@@ -577,6 +577,7 @@ using namespace sp;
 namespace {
 
 constexpr int32_t kMostRows = (1 << 26) - 4;                // a wave each, and a grid has fewer than 2^32 threads
+constexpr int32_t kMostWidth = INT32_MAX - 2048;            // (a wave forms the offsets of 64 units of 16 elements behind a row's last one)
 constexpr int32_t kMostWidthIn = 131072;                    // 131072 * 127 * 127 < 2^31
 size_t codes_row(int32_t width_in) { return ((size_t)width_in + 127) / 128 * 128; }
 size_t codes_bytes(int32_t tokens, int32_t width_in) { return ((size_t)tokens * codes_row(width_in) + 255) / 256 * 256; }
@@ -589,7 +590,7 @@ int sp_quantize_int8(const void* x, int64_t x_row, int32_t dtype, int32_t rows, 
                      float* scales, void* hip_stream)
 {
     if (dtype != SP_DTYPE_FP32 && dtype != SP_DTYPE_BF16) return SP_EINVAL;
-    if (rows < 0 || rows > kMostRows || width < 1 || width > INT32_MAX - 16 || (rows > 1 && (x_row < 0 || c_row < width))) return SP_ESHAPE;
+    if (rows < 0 || rows > kMostRows || width < 1 || width > kMostWidth || (rows > 1 && (x_row < 0 || c_row < width))) return SP_ESHAPE;
     if (rows == 0) return SP_OK;
     if (!x || !codes || !scales || ((uintptr_t)x & (dtype == SP_DTYPE_FP32 ? 3 : 1)) || ((uintptr_t)scales & 3)) return SP_EINVAL;
     return launch_quantize_int8(x, x_row, dtype, rows, width, codes, c_row, width, scales, (hipStream_t)hip_stream) == hipSuccess ? SP_OK

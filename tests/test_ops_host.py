@@ -53,6 +53,12 @@ def test_quantize_refuses():
     assert call(P, 8, 0, 1 << 26, 8, P, 8, P, None) == ESHAPE
 
 
+@pytest.mark.parametrize("width", [(1 << 31) - 1, (1 << 31) - 17, (1 << 31) - 1024, (1 << 31) - 2048])
+def test_quantize_refuses_rows_whose_units_pass_32_bits(width):
+    """64 units of 16 elements behind the row's end are still formed in 32 bits."""
+    assert LIB.sp_quantize_int8(P, width, 1, 1, width, P, width, P, None) == ESHAPE
+
+
 def rotary(**k):
     a = dict(x=P, xt=128, xh=64, out=2 * P, ot=128, oh=64, dtype=0, tokens=4, heads=2, width=64, dim=64, layout=0, f=3 * P, factor=1.0,
              pos=4 * P, cu=None, batch=0) | k
