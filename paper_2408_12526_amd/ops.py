@@ -5,7 +5,7 @@ Argument marshalling and checks only: torch supplies device memory and streams, 
 is no fallback.  A call runs on the current stream of the tensors' device, allocates its outputs and workspace from torch's
 allocator, waits for nothing and can be captured in a graph.  What torch must know for the kernels to stay inside the tensors (shapes,
 types, devices, strides) is checked here and raises ValueError; what the library refuses raises sp.SpError.  None has a
-gradient: inputs that require one are refused while gradients are recorded.
+gradient: inputs that require one are refused while gradients are recorded, inputs with a tangent (forward mode) always.
 """
 from __future__ import annotations
 
@@ -67,6 +67,7 @@ def _need(ok: bool, what: str) -> None:
 
 _raw_stream = torch._C._cuda_getCurrentRawStream
 _recording = torch.is_grad_enabled
+_forward_ad = torch.autograd.forward_ad
 _bytes_of = functools.lru_cache(maxsize=4096)(_lib.sp_linear_int8_workspace_bytes)
 
 
@@ -74,6 +75,10 @@ def _home(first: torch.Tensor, *others) -> int:
     """The index of the device that all tensors are on."""
     dev = first.get_device()
     _need(dev >= 0, "the tensors have to be on a GPU: there is no CPU path in this library")
+    if _forward_ad._current_level >= 0:
+        for t in (first, *others):
+            if t is not None and t.is_floating_point() and _forward_ad.unpack_dual(t).tangent is not None:
+                raise ValueError("this operator has no gradient: call it on detached tensors")
     recording = _recording()
     if recording and first.requires_grad:
         raise ValueError("this operator has no gradient: call it under torch.no_grad() or on detached tensors")

@@ -623,6 +623,31 @@ def test_another_stream():
     assert all(torch.equal(g, want) for g in got)
 
 
+def test_tangents_are_refused():
+    """Forward-mode differentiation: a tangent would be lost in silence; tensors without one are taken inside a dual level too."""
+    rng = np.random.default_rng(20)
+    w, ws = weights(rng, 8, 32)
+    x, q = torch.ones(4, 32, device="cuda"), torch.ones(4, 2, 64, device="cuda")
+    f, cu = dev(ops.rotary_frequencies(64)[0]), dev(np.array([0, 4], np.int32))
+    slopes = torch.ones(2, device="cuda")
+    ad = torch.autograd.forward_ad
+
+    def calls(d):
+        return [lambda: ops.quantize_int8(d(x)), lambda: ops.linear_int8(d(x), w, ws), lambda: ops.linear_int8(x, w, d(ws)),
+                lambda: ops.linear_int8(x, w, ws, residual=d(torch.ones(4, 8, device="cuda"))), lambda: ops.rotary(d(q), f, cu_seqlens=cu),
+                lambda: ops.rotary(q, d(f), cu_seqlens=cu), lambda: ops.attention(q, q.clone(), d(q), cu, 4),
+                lambda: ops.attention(q, q.clone(), q.clone(), cu, 4, slopes=d(slopes))]
+
+    with ad.dual_level():
+        for call in calls(lambda t: ad.make_dual(t, torch.ones_like(t))):
+            with pytest.raises(ValueError, match="gradient"):
+                call()
+            with torch.no_grad(), pytest.raises(ValueError, match="gradient"):
+                call()
+        for call in calls(lambda t: ad.make_dual(t, torch.ones_like(t)).detach()) + calls(lambda t: t):
+            call()
+
+
 # ---- refusals ---------------------------------------------------------------------------------------------------
 
 def test_refusals():
