@@ -216,6 +216,9 @@ class Students:
         for t, dtype, shape in ((rotary_frequencies, torch.float64, None), (slopes, torch.float32, (K, A)), (bias, torch.float32, None)):
             if t is not None and (t.dtype != dtype or t.device != self.device or not t.is_contiguous() or (shape and tuple(t.shape) != shape)):
                 raise ValueError(f"a contiguous {dtype} tensor on {self.device} is wanted" + (f" of shape {shape}" if shape else ""))
+        layout = {"half": 0, "interleaved": 1}.get(rotary_layout)
+        if layout is None:
+            raise ValueError("rotary_layout: half or interleaved")
         if rotary_frequencies is not None and rotary_frequencies.dim() != 1:
             raise ValueError("rotary_frequencies: [rotated elements of a head / 2] is wanted")
         if bias is not None and (bias.dim() != 3 or tuple(bias.shape[:2]) != (K, A) or bias.shape[2] % 2 == 0):
@@ -223,7 +226,7 @@ class Students:
         plain = rotary_frequencies is None and cap <= 0 and window is None and slopes is None and bias is None
         left, right = (-1, -1) if window is None else window
         form = sp_attention_form(
-            2 * rotary_frequencies.numel() if rotary_frequencies is not None else 0, {"half": 0, "interleaved": 1}[rotary_layout],
+            2 * rotary_frequencies.numel() if rotary_frequencies is not None else 0, layout,
             rotary_frequencies.data_ptr() if rotary_frequencies is not None else None, rotary_factor, cap, left, right,
             slopes.data_ptr() if slopes is not None else None, bias.data_ptr() if bias is not None else None,
             bias.shape[2] // 2 if bias is not None else 0)

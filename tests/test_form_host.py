@@ -76,3 +76,10 @@ def test_a_captured_form_stays(students, call):
     del old, f
     gc.collect()
     assert all(r() is not None for r in refs) and len(students._kept_forms) == 1
+
+
+def test_an_unknown_layout_is_a_value_error(students):
+    for more in ({}, form()):
+        with pytest.raises(ValueError, match="rotary_layout"):
+            students.set_attention_form(rotary_layout="other", **more)
+    assert students._form is None
