@@ -117,6 +117,12 @@ def _call(dev: int, fn, *args) -> None:
         raise SpError(rc)
 
 
+def _fit(*sizes: int) -> None:
+    """Sizes that the library takes as 32-bit numbers."""
+    if max(sizes) > 0x7fffffff:
+        raise ValueError(f"sizes of 2^31 and more are not taken: {sizes}")
+
+
 def _dtype(t: torch.Tensor) -> int:
     d = _DTYPES.get(t.dtype)
     if d is None:
@@ -150,6 +156,7 @@ def quantize_int8(x: torch.Tensor):
     dtype, dev = _dtype(x), _home(x)
     _need(x.dim() == 2 and x.shape[1] >= 1, "x: a matrix is wanted")
     rows, width = x.shape
+    _fit(rows, width)
     x_row = _rows(x, "x", x.shape, x.dtype)
     pad = (width + 15) // 16 * 16
     codes = torch.empty(rows, pad, dtype=torch.int8, device=x.device)
@@ -169,6 +176,7 @@ def linear_int8(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, bias
     _need(x.dim() == 2 and codes.dim() == 2, "x and codes: matrices are wanted")
     T, K = x.shape
     N, Kw = codes.shape
+    _fit(T, K, N)
     _need(codes.dtype is torch.int8 and Kw == K, "codes: int8 [width_out, width_in] is wanted")
     _need(K >= 1 and N >= 1, "codes: at least one row and one column are wanted")
     pad = (K + 15) // 16 * 16
@@ -221,6 +229,7 @@ def rotary(x: torch.Tensor, frequencies: torch.Tensor, *, positions: torch.Tenso
     _need(way is not None, "layout: half or interleaved")
     _need((positions is None) != (cu_seqlens is None), "positions or cu_seqlens: one of the two")
     T, A, D = x.shape
+    _fit(T, A, D)
     x_token, x_head, one = x.stride()
     _need(one == 1, "x: the elements of a head have to be contiguous")
     half = frequencies.numel()

@@ -8,6 +8,7 @@ calling it without a GPU, raises.
 from __future__ import annotations
 
 import ctypes as C
+import operator
 import os
 
 import numpy as np
@@ -224,7 +225,12 @@ class Students:
         if bias is not None and (bias.dim() != 3 or tuple(bias.shape[:2]) != (K, A) or bias.shape[2] % 2 == 0):
             raise ValueError(f"bias: [{K}, {A}, 2 reach + 1] is wanted")
         plain = rotary_frequencies is None and cap <= 0 and window is None and slopes is None and bias is None
-        left, right = (-1, -1) if window is None else window
+        try:
+            left, right = (-1, -1) if window is None else (max(-1, operator.index(w)) for w in window)
+        except TypeError:
+            raise ValueError("window: two whole numbers are wanted") from None
+        if max(left, right) > 0x7fffffff:
+            raise ValueError("window: bounds below 2^31 are wanted (-1: none)")
         form = sp_attention_form(
             2 * rotary_frequencies.numel() if rotary_frequencies is not None else 0, layout,
             rotary_frequencies.data_ptr() if rotary_frequencies is not None else None, rotary_factor, cap, left, right,

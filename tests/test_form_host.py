@@ -83,3 +83,12 @@ def test_an_unknown_layout_is_a_value_error(students):
         with pytest.raises(ValueError, match="rotary_layout"):
             students.set_attention_form(rotary_layout="other", **more)
     assert students._form is None
+
+
+@pytest.mark.parametrize("window", [(1 << 32, 3), (3, (1 << 31)), (1.5, 2), (None, 2)])
+def test_windows_that_do_not_fit_are_refused(students, window):
+    """They would lose their upper bits: 2^32 keys to the left would be none."""
+    with pytest.raises(ValueError, match="window"):
+        students.set_attention_form(window=window)
+    for good in (((1 << 31) - 1, -1), (-(1 << 40), 0)):
+        students.set_attention_form(window=good)

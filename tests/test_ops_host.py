@@ -144,6 +144,27 @@ def test_attention_holds_its_workspace_through_the_call(monkeypatch):
     assert seen == [True]
 
 
+def test_sizes_that_leave_32_bits_are_refused(monkeypatch):
+    """Views of one element as 2^32 + 5 rows or columns: the library would see five of them."""
+    monkeypatch.setattr(ops, "_home", lambda *a: 0)
+    monkeypatch.setattr(ops, "_call", lambda *a: pytest.fail("the call was made"))
+    monkeypatch.setattr(torch.Tensor, "new_empty", lambda t, shape: t[:1, :1].expand(shape))
+    monkeypatch.setattr(ops.torch, "empty", lambda *shape, **k: torch.zeros(1, dtype=k["dtype"]).expand(shape if len(shape) > 1 else 1))
+    far = (1 << 32) + 5
+    one, code = torch.ones(1, 16), torch.ones(1, 16, dtype=torch.int8)
+    with pytest.raises(ValueError):
+        ops.quantize_int8(one.expand(far, 16))
+    with pytest.raises(ValueError):
+        ops.linear_int8(one.expand(far, 16), code, torch.ones(1))
+    x = torch.ones(1, 1, 64)
+    with pytest.raises(ValueError):
+        ops.rotary(x.expand(far, 1, 64), torch.ones(32, dtype=torch.float64), cu_seqlens=torch.zeros(2, dtype=torch.int32))
+    with pytest.raises(ValueError):
+        ops.rotary(x.expand(1, far, 64), torch.ones(32, dtype=torch.float64), cu_seqlens=torch.zeros(2, dtype=torch.int32))
+    with pytest.raises(ValueError):
+        ops.attention(x.expand(far, 1, 64), x, x, torch.zeros(2, dtype=torch.int32), 1, torch.zeros(2, dtype=torch.int32), 1)
+
+
 # ---- frequencies ------------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("dim", [2, 4, 40, 64, 128])
