@@ -1,4 +1,5 @@
 """The operators of include/sp_ops.h on the GPU against the 64-bit oracle (bounds are derived there, not fitted)."""
+import ctypes
 import itertools
 import math
 
@@ -521,6 +522,74 @@ def test_attention_inconsistent_offsets_stay_inside():
         ops.attention(q, k, v, dev(np.array(cu, np.int32)), 30)
         ops.attention(q[:1].contiguous(), k, v, dev(np.array([0, 1], np.int32)), 1, dev(np.array(cu, np.int32)), 64)
     torch.cuda.synchronize()
+
+
+class Guarded:
+    """Device memory of n elements between two stretches that nobody may write."""
+    EDGE, FILL = 1 << 16, 0xA5
+
+    def __init__(self, n, dtype, value=None):
+        size = n * torch.empty(0, dtype=dtype).element_size()
+        self.all = torch.full((2 * self.EDGE + (size + 255) // 256 * 256,), self.FILL, dtype=torch.uint8, device="cuda")
+        self.bytes = self.all[self.EDGE: self.EDGE + size]
+        self.t = self.bytes.view(dtype)
+        if value is not None:
+            self.t.copy_(value.reshape(-1))
+
+    def intact(self):
+        return bool((self.all[: self.EDGE] == self.FILL).all()) and bool((self.all[self.EDGE + len(self.bytes):] == self.FILL).all())
+
+
+def clamped(cu, total, most):
+    """The sequences of offsets that need not be any."""
+    out = []
+    for a, z in zip(cu[:-1], cu[1:]):
+        at = min(max(a, 0), total)
+        out.append((at, at + min(max(z - at, 0), most, total - at)))
+    return out
+
+
+BAD_OFFSETS = {"beyond": lambda n: [0, n // 2, 1 << 30], "negative": lambda n: [-7, n // 2, n], "falling": lambda n: [n, n // 2, 0],
+               "far": lambda n: [0, 1 << 30, n // 2], "outside": lambda n: [n + 5, n + 9, n + 20], "all": lambda n: [-(1 << 30), 5, (1 << 31) - 1]}
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("docs", [False, True])
+@pytest.mark.parametrize("total_q,max_q,total_k", [(4, 2, 100), (4, 2, 6000), (70, 40, 90), (300, 160, 310), (300, 160, 6000)])
+@pytest.mark.parametrize("kind", BAD_OFFSETS)
+def test_attention_inconsistent_offsets_touch_nothing_else(dtype, docs, total_q, max_q, total_k, kind):
+    """Offsets that point outside, fall, or exceed the bounds, in calls of few and many rows, split over the keys or not: what stands around the
+    output, lse and the workspace stays; with sound offsets of the queries each of them sees the clamped keys."""
+    rng = np.random.default_rng(21)
+    A, D, T = 2, 64, TYPES[dtype]
+    max_k = total_k * 2 // 3
+    q, k, v = (Guarded(n * A * D, T, dev(rng.standard_normal((n, A, D)).astype(np.float32), dtype)) for n in (total_q, total_k, total_k))
+    dq, dk = (Guarded(n, torch.int32, dev(rng.integers(-1, 2, n).astype(np.int32))) for n in (total_q, total_k))
+    sound = [0, max_q, total_q]
+    for cu_q, cu_k in ((sound, BAD_OFFSETS[kind](total_k)), (BAD_OFFSETS[kind](total_q), [0, total_k // 2, total_k]),
+                       (BAD_OFFSETS[kind](total_q), BAD_OFFSETS[kind](total_k))):
+        out, lse = Guarded(total_q * A * D, T), Guarded(total_q * A, torch.float32)
+        at = [Guarded(3, torch.int32, dev(np.array(c, np.int32))) for c in (cu_q, cu_k)]
+        a = ops.sp_attention_args(
+            q=q.t.data_ptr(), k=k.t.data_ptr(), v=v.t.data_ptr(), out=out.t.data_ptr(), lse=lse.t.data_ptr(), q_token=A * D, q_head=D, k_token=A * D,
+            k_head=D, v_token=A * D, v_head=D, out_token=A * D, out_head=D, cu_q=at[0].t.data_ptr(), cu_k=at[1].t.data_ptr(), dtype=sp.SP_DTYPE_BF16 if
+            dtype == "bf16" else sp.SP_DTYPE_FP32, batch=2, heads=A, kv_heads=A, width=D, total_q=total_q, total_k=total_k, max_q=max_q, max_k=max_k,
+            scale=0.125, left=-1, right=-1, doc_q=dq.t.data_ptr() if docs else None, doc_k=dk.t.data_ptr() if docs else None)
+        need = sp.raw_lib().sp_attention_workspace_bytes(ctypes.addressof(a))
+        assert (need > 0) == (total_k == 6000)
+        ws = Guarded(need, torch.uint8)
+        assert sp.raw_lib().sp_attention(ctypes.addressof(a), ws.t.data_ptr(), need, torch.cuda.current_stream().cuda_stream) == 0
+        torch.cuda.synchronize()
+        assert all(g.intact() for g in (q, k, v, dq, dk, out, lse, ws, *at))
+        if cu_q is not sound:
+            continue
+        qh, kh, vh = (host(t.t.view(-1, A, D)) for t in (q, k, v))
+        qd, kd = dq.t.cpu().numpy(), dk.t.cpu().numpy()
+        for (q0, q1), (k0, k1) in zip(clamped(cu_q, total_q, max_q), clamped(cu_k, total_k, max_k)):
+            of = dict(doc_q=qd[q0:q1], doc_k=kd[k0:k1]) if docs else {}
+            want, wl, ob, lb = oracle.attention(qh[q0:q1], kh[k0:k1], vh[k0:k1], [0, q1 - q0], [0, k1 - k0], dtype=dtype, **of)
+            near(out.t.view(-1, A, D)[q0:q1], want, ob, "out")
+            near(lse.t.view(-1, A)[q0:q1], wl, lb, "lse")
 
 
 # ---- together ---------------------------------------------------------------------------------------------------
