@@ -371,7 +371,7 @@ hipError_t launch_tile(const Int8Args& a, hipStream_t s)
 
 // ---- few tokens ---------------------------------------------------------------------------------------------------
 
-// Up to 16 TB tokens: a workgroup takes 16 channels, its four waves the k-tiles of 128 codes in turn, straight from memory to the registers
+// Up to 16 TB tokens of one group: a workgroup takes 16 channels, its four waves the k-tiles of 128 codes in turn, straight from memory to the registers
 // (v_mfma_i32_16x16x64_i8; a row's 64 contiguous bytes per load), and adds the waves' sums at the end.  What counts is the time of one trip
 // to memory: four k-tiles are requested at a time.  FUSED (TB = 1): the workgroup quantises the rows itself, into LDS, while its weights are
 // under way; one launch instead of two.
@@ -391,9 +391,8 @@ __global__ __launch_bounds__(256) void few_int8_kernel(Int8Args p, FewArgs f)
     __shared__ float scales[16];
     typedef int i32x4 __attribute__((ext_vector_type(4)));
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l15 = lane & 15, kq = lane >> 4;
-    const int n0 = blockIdx.x * 16, m = blockIdx.y, nk = (p.Kd + 127) >> 7, last = (p.Kd - 1) & ~15;
-    const int8_t* W = p.W + (size_t)m * p.w_ss + (size_t)(n0 + l15 < p.N ? n0 + l15 : p.N - 1) * p.w_row;
-    const int8_t* A = p.A + (size_t)m * p.a_ss;
+    const int n0 = blockIdx.x * 16, nk = (p.Kd + 127) >> 7, last = (p.Kd - 1) & ~15;
+    const int8_t* W = p.W + (size_t)(n0 + l15 < p.N ? n0 + l15 : p.N - 1) * p.w_row;
     constexpr int AHEAD = TB == 4 ? 2 : 4;
     v4i w[AHEAD][2], a[AHEAD][2][TB];
     auto load_w = [&](int i, int kt) {
@@ -410,7 +409,7 @@ __global__ __launch_bounds__(256) void few_int8_kernel(Int8Args p, FewArgs f)
             for (int b = 0; b < TB; ++b) {
                 const int tok = b * 16 + l15, k = kt * 128 + s * 64 + kq * 16;
                 if (FUSED) a[i][s][b] = *(const v4i*)((const char*)smem + (size_t)tok * f.pitch + k);
-                else a[i][s][b] = *(const v4i*)(A + (size_t)(tok < p.tokens ? tok : p.tokens - 1) * p.a_row + k);
+                else a[i][s][b] = *(const v4i*)(p.A + (size_t)(tok < p.tokens ? tok : p.tokens - 1) * p.a_row + k);
             }
     };
     i32x4 acc[TB];
@@ -444,17 +443,15 @@ __global__ __launch_bounds__(256) void few_int8_kernel(Int8Args p, FewArgs f)
     barrier_lds();
     const int n = n0 + (tid & 15);
     if (n >= p.N) return;
-    const float sw = ((const float*)((const char*)p.w_scales + m * p.ws_ss))[n];
-    const float bias = p.bias ? ((const float*)((const char*)p.bias + m * p.b_ss))[n] : 0.f;
-    const float* sa = (const float*)((const char*)p.a_scales + m * p.as_ss);
+    const float sw = p.w_scales[n], bias = p.bias ? p.bias[n] : 0.f;
 #pragma unroll
     for (int b = 0; b < TB; ++b) {
         const int tok = b * 16 + (tid >> 4);
         if (tok >= p.tokens) break;
         const int sum = sums[0][b][tid] + sums[1][b][tid] + sums[2][b][tid] + sums[3][b][tid];
-        const float st = FUSED ? scales[tok] : sa[tok];
-        const float res = EPI == SP_LINEAR_RESIDUAL ? (float)((const E*)((const char*)p.res + m * p.res_ss))[tok * p.res_row + n] : 0.f;
-        ((E*)((char*)p.out + m * p.out_ss))[tok * p.out_row + n] = (E)finish<EPI>(sum, st * sw, bias, res);
+        const float st = FUSED ? scales[tok] : p.a_scales[tok];
+        const float res = EPI == SP_LINEAR_RESIDUAL ? (float)((const E*)p.res)[tok * p.res_row + n] : 0.f;
+        ((E*)p.out)[tok * p.out_row + n] = (E)finish<EPI>(sum, st * sw, bias, res);
     }
 }
 
@@ -472,7 +469,7 @@ hipError_t launch_few(const Int8Args& a, const QuantArgs& q, hipStream_t s)
             raised.store(true, std::memory_order_release);
         }
     }
-    hipLaunchKernelGGL(kern, dim3((unsigned)((a.N + 15) / 16), (unsigned)a.groups), dim3(256), smem, s, a, f);
+    hipLaunchKernelGGL(kern, dim3((unsigned)((a.N + 15) / 16)), dim3(256), smem, s, a, f);
     return hipGetLastError();
 }
 
@@ -501,10 +498,11 @@ hipError_t launch_tiles(const Int8Args& a, hipStream_t s)
 template <class E, int EPI>
 hipError_t launch_epilogue(const Int8Args& a, hipStream_t s)
 {
+    // (students side by side come with at least 2048 rows each)
+    if (a.tokens > kFewTokens || a.groups > 1) return launch_tiles<E, EPI>(a, s);
     if (a.tokens <= 16) return launch_few<1, false, E, EPI>(a, QuantArgs{}, s);
     if (a.tokens <= 32) return launch_few<2, false, E, EPI>(a, QuantArgs{}, s);
-    if (a.tokens <= kFewTokens) return launch_few<4, false, E, EPI>(a, QuantArgs{}, s);
-    return launch_tiles<E, EPI>(a, s);
+    return launch_few<4, false, E, EPI>(a, QuantArgs{}, s);
 }
 
 template <class E>
