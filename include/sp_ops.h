@@ -89,8 +89,8 @@ int sp_rotary(const void* x, int64_t x_token, int64_t x_head, void* out, int64_t
  *     out = sum_j softmax_j(s) v_j,   lse = ln sum_j exp(s)          over the visible j
  * j is visible where (-left <= d <= right, a negative bound being none, or j < prefix[b]) and, with documents, doc_q = doc_k >= 0.
  * A bias of minus infinity hides a key too (finite ones below -2e38 weigh like -2e38); positions beyond +-2^30 count as that.  A query
- * that sees nothing gets zeros and lse = minus infinity; one that holds a NaN and sees a key gets NaN in both.  Sums and statistics are
- * fp32; bf16 rounds the probabilities to bf16 before their product with the values, and the result.
+ * that sees nothing gets zeros and lse = minus infinity; one that holds a NaN and sees a key, or sees one whose bias is NaN, gets NaN in
+ * both.  Sums and statistics are fp32; bf16 rounds the probabilities to bf16 before their product with the values, and the result.
  * Keys behind a sequence's end and, with documents, keys of a negative document may hold anything; a visible key of one query must be
  * finite also where the mask hides it from another.
  * Rows of out and lse that belong to no sequence are left as they were.  causal attention is right = 0. */

@@ -90,8 +90,8 @@ __device__ __forceinline__ void sequence_range(int t0, int t1, int total, int mo
     n = n > total - at ? total - at : n;
 }
 
-// A bias in units of the base-2 logarithm; finite ones stay finite.
-__device__ __forceinline__ float in_log2(float b) { return __builtin_isinf(b) ? b : __builtin_amdgcn_fmed3f(b * kLog2e, -3.0e38f, 3.0e38f); }
+// A bias in units of the base-2 logarithm; finite ones stay finite, infinities and NaN what they are.
+__device__ __forceinline__ float in_log2(float b) { return __builtin_isfinite(b) ? __builtin_amdgcn_fmed3f(b * kLog2e, -3.0e38f, 3.0e38f) : b; }
 
 // From a row's reference (base-2 units) and sum: zero where it has seen nothing, else one at least, or NaN, which stays NaN.
 __device__ __forceinline__ float lse_of(float top, float sum) { return sum == 0.f ? -INFINITY : (top + __builtin_log2f(sum)) * kLn2; }

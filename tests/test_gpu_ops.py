@@ -451,6 +451,29 @@ def test_attention_caps_of_any_size(dtype, cap, nq):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("reach", [9, 3000])
+@pytest.mark.parametrize("where", ["inside", "left", "right"])
+@pytest.mark.parametrize("nq,nk", [([1, 2], [300, 40]), ([40, 50], [40, 50]), ([300, 2], [300, 9])])
+def test_attention_biases_that_are_nan(dtype, reach, where, nq, nk):
+    """A NaN in the table is in the result of every query that sees a key at its distance, and in nothing else."""
+    rng = np.random.default_rng(22)
+    q, k, v, cq, ck = batch_of(rng, dtype, nq, nk, 2, 1, 64)
+    bias = rng.standard_normal((2, 2 * reach + 1)).astype(np.float32)
+    bad = {"inside": -5, "left": -reach, "right": reach}[where]
+    want, wl, ob, lb = oracle.attention(host(q), host(k), host(v), cq, ck, dtype=dtype, bias=bias, left=20, right=12)
+    hit = np.zeros(int(cq[-1]), bool)
+    for a0, a1, n in zip(cq[:-1], cq[1:], nk):
+        d = np.arange(n)[None] - (n - (a1 - a0) + np.arange(a1 - a0))[:, None]
+        hit[a0:a1] = ((np.clip(d, -reach, reach) == bad) & (d >= -20) & (d <= 12)).any(1)
+    assert reach == 3000 and where != "inside" or hit.any() or where == "right"
+    want[hit, 1] = wl[hit, 1] = math.nan
+    bias[1, reach + bad] = math.nan
+    got, lse = ops.attention(q, k, v, dev(cq), max(nq), dev(ck), max(nk), bias=dev(bias), window=(20, 12), with_lse=True)
+    near(got, want, ob, "out")
+    near(lse, wl, lb, "lse")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_attention_extreme_scores(dtype):
     """Scores so far apart that one key takes all, and scores near the lowest value of the type."""
     rng = np.random.default_rng(7)
