@@ -183,7 +183,8 @@ int sp_forward_static(const sp_model* model, const int32_t* token_ids, const int
 
 /* Another form of attention for all layers of a loaded group, in place of softmax(q k^T / 8) v over all tokens of a sequence: rotary
  * positions, capped scores, a window, and biases by distance, as defined with sp_rotary and sp_attention in sp_ops.h
- * (scale 1/8, queries and keys of a sequence being the same tokens).  Null: back to the plain form.
+ * (scale 1/8, queries and keys of a sequence being the same tokens; rotated queries and keys are rounded to the path's type twice, as the projection's
+ * result and once more).  Null: back to the plain form.
  * The arrays are device memory of the caller, read by every forward until the form is replaced or the group freed.  Not to be called
  * while a call on the model is being issued by another thread; calls issued before keep the form they were issued with, and need its arrays until
  * they are done: a call captured in a graph for as long as the graph is replayed.

@@ -34,7 +34,7 @@ int sp_quantize_int8(const void* x, int64_t x_row, int32_t dtype, int32_t rows, 
                      int64_t c_row, float* scales, void* hip_stream);
 
 /* out[t][n] = epilogue(s[t] w_scales[n] sum_k c[t][k] w_codes[n][k] + bias[n]), c and s as above from the rows of x, the sum in
- * integers (exact), the rest in fp32, rounded once to dtype.
+ * integers (exact), the rest in fp32 (s[t] w_scales[n] first: it has to stay inside that type), rounded once to dtype.
  *   x         [tokens][width_in], row stride x_row           out  [tokens][width_out], row stride out_row; not x
  *   w_codes   [width_out][width_in], row stride w_row: a multiple of 16, 16-byte aligned, every row readable up to the next
  *             multiple of 16 of width_in (what stands there does not count); -128 is not a code

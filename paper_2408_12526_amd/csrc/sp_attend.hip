@@ -17,7 +17,7 @@
 // SIMD.  bf16, 16 heads, 4 x 4096 tokens: width 128 on 4 key heads 660 us (830 TFLOP/s), causal 359, capped 786; width 64 361 (760), with slopes 429.
 // With few rows the read of the keys and values: 8 queries of 32 heads on 4 key heads of 128 against 135 k keys, 270 MB, 65 us and 5 for the join (4.1
 // TB/s without it).  Short sequences: the chain from the offsets to the first tile and out again, about 8 us a workgroup: 256 sequences of 57 tokens on
-// average, 12 heads, 41 us.
+// average, 12 heads, 40 us.
 #include <atomic>
 #include <cfloat>
 #include <cmath>
@@ -448,7 +448,7 @@ __global__ __launch_bounds__((Shape<E, DP, KIND>::WAVES * 64), waves_per_simd(si
                 for (int s2 = 0; s2 < 2; ++s2) {
                     bf16x8 pf;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) pf[e] = (bf16)sc[nb][8 * s2 + e];
+                    for (int e = 0; e < 8; ++e) pf[e] = (bf16)sc[nb][8 * s2 + e];     // (half a step each: weights of 32 bits would take twice the products)
 #pragma unroll
                     for (int d = 0; d < ND; ++d) {
                         const char* at = tile + (vat ^ (d * 64)) + (32 * nb + 16 * s2) * RC * 16;
@@ -705,9 +705,10 @@ struct Plan {
 };
 
 // Shape of the workgroups: few rows where no sequence has more than 32, small where they have up to 96 (fp32, whose waves the matrix
-// products keep busy for longer: 192) on average, of 128 rows half the waves being idle then.  us a launch, small / many, width 64: fp32, 8
-// heads, 32 sequences of 158 on average 53 / 68, 2 of 2048 281 / 232; bf16, 16 heads, 64 sequences of 256 46 / 43, 4 of 4096 451 / 366; 12
-// heads, 256 sequences of 57 on average 41 / 57.  Parts of a call: as many as give every compute unit two workgroups, of at least 256 keys for each wave (few
+// products keep busy for longer: 192) on average, of 128 rows half the waves being idle then.  us a call in a graph, small / many, width 64:
+// fp32, 8 heads, 32 sequences of 158 on average 48 / 64, of 128 25 / 25, 192 37 / 47, 224 67 / 54, 2 of 2048 277 / 217; bf16, 16 heads, 64 sequences of 64
+// 13.7 / 13.3, 80 16.8 / 18.2, 96 16.1 / 18.6, 112 19.9 / 19.7, 128 20.2 / 24.2, 192 35 / 31, 256 43 / 40, 4 of 4096 437 / 362; 12 heads, 256 sequences of 57 on
+// average 33 / 41.  Parts of a call: as many as give every compute unit two workgroups, of at least 256 keys for each wave (few
 // rows) or 512 for all of them.
 Plan make_plan(const sp_attention_args& a, int groups, bool split)
 {
