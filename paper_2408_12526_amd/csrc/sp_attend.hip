@@ -829,7 +829,8 @@ int check_attention(const sp_attention_args* a)
     if ((int64_t)a->total_q * a->heads > (1 << 30) || (int64_t)a->batch * a->heads > (1 << 22)) return SP_ESHAPE;
     if (!std::isfinite(a->scale) || !std::isfinite(a->cap) || a->reach < 0 || a->reach > (1 << 20)) return SP_EINVAL;
     if (a->bias && (int64_t)a->heads * (2 * (int64_t)a->reach + 1) > (1 << 30)) return SP_ESHAPE;
-    if (!a->doc_q != !a->doc_k) return SP_EINVAL;
+    // (one of nothing may be null)
+    if ((a->doc_q && !a->doc_k && a->total_k > 0) || (a->doc_k && !a->doc_q && a->total_q > 0)) return SP_EINVAL;
     const int sz = a->dtype == SP_DTYPE_FP32 ? 4 : 2;
     const int64_t strides[] = {a->q_token, a->q_head, a->k_token, a->k_head, a->v_token, a->v_head, a->out_token, a->out_head};
     for (int64_t s : strides) {

@@ -186,13 +186,14 @@ int sp_rotary(const void* x, int64_t x_token, int64_t x_head, void* out, int64_t
     if (layout != SP_ROTARY_HALF && layout != SP_ROTARY_INTERLEAVED) return SP_EINVAL;
     if (tokens < 0 || heads < 1 || heads > 65535 || width < 2 || width > 65536 || dim < 2 || dim % 2 || dim > width) return SP_ESHAPE;
     const uintptr_t low = dtype == SP_DTYPE_FP32 ? 3 : 1;
-    if (!frequencies || ((uintptr_t)frequencies & 7) || (!positions == !cu_seqlens) || ((uintptr_t)positions & 3) || ((uintptr_t)cu_seqlens & 3))
+    if (!frequencies || ((uintptr_t)frequencies & 7) || (positions && cu_seqlens) || ((uintptr_t)positions & 3) || ((uintptr_t)cu_seqlens & 3))
         return SP_EINVAL;
+    if (!positions && !cu_seqlens && tokens > 0) return SP_EINVAL;      // (positions of nothing may be null)
     if (cu_seqlens && batch < 0) return SP_ESHAPE;
     if (x_token < 0 || x_head < 0 || out_token < 0 || out_head < 0) return SP_ESHAPE;
     // (rows of the output that share memory would be written by several threads)
     if (!rows_apart(tokens, out_token, heads, out_head, width)) return SP_ESHAPE;
-    if (x == out && (x_token != out_token || x_head != out_head)) return SP_EINVAL;
+    if (x && x == out && (x_token != out_token || x_head != out_head)) return SP_EINVAL;
     // a thread per piece of a token: the grid holds 2^31 of them at most
     if ((int64_t)tokens * (width / 2 + 1) > INT32_MAX) return SP_ESHAPE;
     if (tokens == 0 || (cu_seqlens && batch == 0)) return SP_OK;

@@ -537,6 +537,20 @@ def test_attention_nothing_to_do():
     assert bool((out == 0).all()) and bool((lse == -math.inf).all())
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("nq", [3, 100])
+def test_empty_tensors_beside_others(dtype, nq):
+    """No tokens to rotate; documents with no queries, and with no keys."""
+    f, none = dev(ops.rotary_frequencies(64)[0]), torch.empty(0, dtype=torch.int32, device="cuda")
+    x, e = torch.ones(nq, 2, 64, dtype=TYPES[dtype], device="cuda"), torch.empty(0, 2, 64, dtype=TYPES[dtype], device="cuda")
+    assert ops.rotary(e, f, positions=none).shape == e.shape and ops.rotary(e, f, cu_seqlens=dev(np.zeros(3, np.int32))).shape == e.shape
+    assert ops.rotary(torch.ones(nq, 6, 64, dtype=TYPES[dtype], device="cuda")[:0, :4], f, positions=none).shape == (0, 4, 64)
+    docs, cu, cu0 = torch.zeros(nq, dtype=torch.int32, device="cuda"), dev(np.array([0, nq], np.int32)), dev(np.zeros(2, np.int32))
+    assert ops.attention(e, x, x, cu0, 0, cu, nq, doc_q=none, doc_k=docs).shape == e.shape
+    out, lse = ops.attention(x, e, e, cu, nq, cu0, 0, doc_q=docs, doc_k=none, with_lse=True)
+    assert bool((out == 0).all()) and bool((lse == -math.inf).all())
+
+
 def test_attention_inconsistent_offsets_stay_inside():
     """Offsets that point outside, fall, or exceed the bounds: clamped, nothing else is promised."""
     rng = np.random.default_rng(11)

@@ -104,6 +104,14 @@ def test_attention_of_nothing():
     assert LIB.sp_attention_workspace_bytes(None) == 0
 
 
+def test_arrays_of_nothing_may_be_null():
+    """Empty tensors have no address."""
+    assert rotary(tokens=0, pos=None, x=None, out=None) == 0 and rotary(tokens=0, pos=None, x=None, out=None, xt=256) == 0
+    assert attend(total_q=0, q=None, out=None, doc_k=P) == 0
+    assert attend(total_k=0, max_k=0, k=None, v=None, doc_q=P, batch=0) == 0
+    assert attend(doc_k=P) == EINVAL and attend(total_k=0, doc_k=P) == EINVAL and attend(total_q=0, doc_q=P) == EINVAL
+
+
 def test_no_cpu_path():
     x = torch.ones(4, 32)
     with pytest.raises(ValueError):
