@@ -561,6 +561,27 @@ def test_attention_inconsistent_offsets_stay_inside():
     torch.cuda.synchronize()
 
 
+@pytest.mark.parametrize("nq", [1, 40])
+def test_attention_offsets_beyond_32_bits(nq):
+    """A cache of more than 4 GiB of keys: a window at its end, and a short sequence behind a long one."""
+    rng = np.random.default_rng(23)
+    n, G, D = 2_200_003, 8, 128
+    assert n * G * D * 2 > 1 << 32
+    k, v = (torch.empty(n, G, D, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    for t in (k, v):
+        t[-1500:] = dev(rng.standard_normal((1500, G, D)).astype(np.float32), "bf16")
+    q = dev(rng.standard_normal((2 * nq, 2 * G, D)).astype(np.float32), "bf16")
+    part = [host(t[-1500:]) for t in (k, v)]
+    got, lse = ops.attention(q[nq:], k, v, dev(np.array([0, nq], np.int32)), nq, dev(np.array([0, n], np.int32)), n, causal=True, window=(700, 0), with_lse=True)
+    want, wl, ob, lb = oracle.attention(host(q[nq:]), *part, [0, nq], [0, 1500], left=700, right=0, dtype="bf16")
+    near(got, want, ob, "out")
+    near(lse, wl, lb, "lse")
+    got, lse = ops.attention(q[nq:], k, v, dev(np.array([0, 0, nq], np.int32)), nq, dev(np.array([0, n - 1000, n], np.int32)), n, with_lse=True)
+    want, wl, ob, lb = oracle.attention(host(q[nq:]), *(t[-1000:] for t in part), [0, nq], [0, 1000], dtype="bf16")
+    near(got, want, ob, "out")
+    near(lse, wl, lb, "lse")
+
+
 class Guarded:
     """Device memory of n elements between two stretches that nobody may write."""
     EDGE, FILL = 1 << 16, 0xA5
